@@ -600,6 +600,228 @@ rtp_status rtp_moe_flush(rtp_moe *moe);
 rtp_status rtp_moe_sync(rtp_moe *moe);
 rtp_ring *rtp_moe_ring(rtp_moe *moe);
 
+/* ---- around a unit: router, combination of experts, norms, optimizer ------ */
+
+/* The operators of a training step that stand around a rotated unit.  They
+ * work on the worker's own tokens and stores, need no ring, and each enqueues
+ * its kernels on `stream` (a stream of the current device, on which all
+ * pointers must be) and returns.  They may be captured into a graph: no
+ * allocation, no clearing by the runtime, no state between calls.  A call that
+ * is refused has enqueued nothing.  Zero tokens are a call that does nothing.
+ * Outputs do not overlap inputs or each other except where that is said. */
+
+/* Scores a router gives its experts.  */
+typedef enum { RTP_SCORE_SOFTMAX = 0, RTP_SCORE_SIGMOID = 1 } rtp_score;
+
+#define RTP_ROUTE_MAX_EXPERTS 1024
+#define RTP_ROUTE_MAX_TOP 32
+#define RTP_ROUTE_MAX_GROUPS 64
+
+/* Routing of T tokens to k of E experts (MoE block item of the RTP
+ * Transformers section names the layer and gives no router).
+ *   s = softmax(logits) over the E experts, or sigmoid(logits);
+ *   choice = s + bias (bias: fp32 [E] or NULL; it balances the load, has no
+ *     part in the weights and gets no gradient);
+ *   groups > 1: the E experts are `groups` runs of equal length; a group's
+ *     score is its largest choice, or with group_top = 2 the sum of its two
+ *     largest; only experts of the kept_groups best groups are eligible;
+ *   ids = the k eligible experts of largest choice, largest first;
+ *   weights = scale * s of those, renormalise != 0: divided by their sum.
+ * Equal choices and equal groups: lowest index first.  With a bias or groups
+ * the choice is made in 64 bits (two choices that 32 bits would round together are kept
+ * apart); without, it is the order of the logits.
+ * A logit of -infinity closes the expert to that token: it ranks behind every
+ * other eligible expert, weighs 0 and has gradient 0 (a token with no open expert gets
+ * weights 0 throughout).  A NaN logit ranks first, and every weight that is
+ * computed with it is NaN (softmax: those of all experts, which then rank alike). */
+typedef struct {
+    int64_t T;
+    int E, k;             /* 1 <= k <= E / groups * kept_groups                   */
+    rtp_score score;
+    int renormalise;
+    float scale;          /* finite                                               */
+    int groups;           /* 1: no groups.  Divides E                             */
+    int kept_groups;      /* 1 .. groups                                          */
+    int group_top;        /* 1 or 2                                               */
+    rtp_dtype dtype;      /* of the logits                                        */
+    rtp_dtype grad_dtype; /* of their gradient (rtp_route_bwd)                    */
+    int64_t ld, ld_grad;  /* elements from one row to the next; 0: E              */
+} rtp_route_desc;
+
+/* logits [T, E] -> ids int32 [T, k], weights fp32 [T, k], both contiguous.
+ * ids are what rtp_moe_fwd takes as route_dev for T * k rows (token t's slots
+ * are rows t * k .. t * k + k - 1).  Errors: RTP_ERR_INVALID (null, bad enum,
+ * scale not finite), RTP_ERR_SHAPE (sizes, leading dimensions, alignment),
+ * RTP_ERR_UNSUPPORTED (more than RTP_ROUTE_MAX_* experts, choices, groups). */
+rtp_status rtp_route_fwd(const rtp_route_desc *d, const void *logits_dev, const float *bias_dev, int32_t *ids_dev,
+                         float *weights_dev, void *stream);
+/* Gradient of the weights dweights fp32 [T, k] -> that of the logits [T, E],
+ * every entry written.  ids: of rtp_route_fwd (the choice itself has no
+ * gradient); ids outside [0, E) have no part in it. */
+rtp_status rtp_route_bwd(const rtp_route_desc *d, const void *logits_dev, const int32_t *ids_dev, const float *dweights_dev,
+                         void *dlogits_dev, void *stream);
+
+#define RTP_COMBINE_MAX_TOP 32
+#define RTP_COMBINE_MAX_D (1 << 20)
+
+/* What the k experts of each token give, weighted: Y[t] = sum over j < k of
+ * weights[t, j] * Yk[t * k + j], summed in fp32 in the order of j and rounded
+ * once.  Yk [T * k, D], Y [T, D] of `dtype`, weights fp32 [T, k] contiguous or
+ * NULL (all 1: the gradient of an expansion).  A slot of weight 0 is not
+ * looked at, whatever it holds (padding, a closed expert).  ld_*: elements from one row to the next,
+ * 0: D. */
+rtp_status rtp_combine_fwd(int64_t T, int k, int64_t D, rtp_dtype dtype, const void *Yk_dev, int64_t ld_yk,
+                           const float *weights_dev, void *Y_dev, int64_t ld_y, void *stream);
+/* Gradients: dYk[t * k + j] = weights[t, j] * dY[t] (zero where the weight is
+ * 0), dweights[t, j] = <dY[t], Yk[t * k + j]> in fp32.  dYk or dweights may be NULL; Yk
+ * is needed for dweights only.  Without weights, dYk is the expansion of the
+ * rows of dY into k slots each (what a unit over T * k rows takes). */
+rtp_status rtp_combine_bwd(int64_t T, int k, int64_t D, rtp_dtype dtype, const void *dY_dev, int64_t ld_dy,
+                           const void *Yk_dev, int64_t ld_yk, const float *weights_dev, void *dYk_dev, int64_t ld_dyk,
+                           float *dweights_dev, void *stream);
+
+typedef enum { RTP_NORM_RMS = 0, RTP_NORM_LAYER = 1 } rtp_norm;
+typedef enum { RTP_GATE_NONE = 0, RTP_GATE_CHANNEL = 1, RTP_GATE_ELEMENT = 2 } rtp_gate;
+#define RTP_NORM_JOIN 1u /* a branch y joins the residual stream: r is written      */
+#define RTP_NORM_POST 2u /* y is normalised before it joins (with RTP_NORM_JOIN)    */
+#define RTP_NORM_PRE 4u  /* the stream is normalised for the next unit: h           */
+#define RTP_NORM_MAX_D (1 << 20)
+
+/* What lies between two units of a residual stream, in one pass over it:
+ *   r = res_scale * x + out_scale * gate . N_post(y)     (RTP_NORM_JOIN)
+ *   h = N_pre(r)                                         (RTP_NORM_PRE; without
+ *                                                         JOIN h = N_pre(x))
+ *   N(v) = (v - mean) / sqrt(var + eps) * w + b     RTP_NORM_LAYER
+ *   N(v) = v / sqrt(mean of v^2 + eps) * w + b      RTP_NORM_RMS
+ * over rows of D; w NULL: 1, b NULL: 0; without RTP_NORM_POST N_post(y) = y.
+ * The stream (x, r) is of stream_dtype, the units' side (y, h, an
+ * RTP_GATE_ELEMENT gate [T, D]) of dtype; w, b and an RTP_GATE_CHANNEL gate
+ * [D] are fp32.  stream_dtype is dtype or RTP_F32.  Arithmetic is fp32; r is
+ * rounded once, and h is the norm of r as it is stored, so that the backward
+ * pass, which reads r, differentiates what was computed. */
+typedef struct {
+    int64_t T, D;            /* 1 <= D <= RTP_NORM_MAX_D                            */
+    rtp_norm kind;
+    unsigned parts;          /* RTP_NORM_*: JOIN, PRE or both; POST with JOIN       */
+    rtp_gate gate;           /* with JOIN                                           */
+    rtp_dtype stream_dtype, dtype;
+    float eps;               /* > 0                                                 */
+    float res_scale, out_scale;
+    const float *w_post_dev, *b_post_dev, *w_pre_dev, *b_pre_dev; /* [D] each, or NULL */
+    const void *gate_dev;
+    int64_t ld_gate;         /* of an element gate; every ld: elements, 0: D        */
+} rtp_norm_desc;
+
+/* x, y -> r, h.  stats: fp32 [T, 4], (mean, 1 / deviation) of y's and of r's
+ * row, for the backward pass (those of a part that is left out are not
+ * written).  r may be x (same ld_*): each row is read before it is written.
+ * Pointers of parts that are left out are not looked at. */
+typedef struct {
+    const void *x_dev, *y_dev;
+    void *r_dev, *h_dev;
+    float *stats_dev;
+    int64_t ld_x, ld_y, ld_r, ld_h;
+} rtp_norm_io;
+rtp_status rtp_norm_fwd(const rtp_norm_desc *d, const rtp_norm_io *io, void *stream);
+
+/* dr (the stream's gradient from what follows; NULL: none), dh -> dx, dy and
+ * the parameters' gradients.  r: the forward pass's (without JOIN: x); y and r
+ * as they were.  An element gate's gradient goes to dgate [T, D] of dtype, a
+ * channel gate's to dgate [D] fp32.  Parameter gradients that are NULL are not computed;
+ * accumulate != 0 adds to what the fp32 ones hold (they travel with nobody:
+ * one set a unit), 0 overwrites.  ws: rtp_norm_ws_bytes() of device memory,
+ * 16-byte aligned, used by this call alone until it is done.  The sums over
+ * rows are in a fixed order: a call repeats bit for bit.
+ * dx may be dr (same ld_*). */
+typedef struct {
+    const void *r_dev, *y_dev, *dr_dev, *dh_dev;
+    const float *stats_dev;
+    void *dx_dev, *dy_dev;
+    void *dgate_dev;
+    float *dw_post_dev, *db_post_dev, *dw_pre_dev, *db_pre_dev; /* [D] each */
+    int accumulate;
+    void *ws_dev;
+    size_t ws_bytes;
+    int64_t ld_r, ld_y, ld_dr, ld_dh, ld_dx, ld_dy, ld_dgate;
+} rtp_norm_grads;
+size_t rtp_norm_ws_bytes(const rtp_norm_desc *d); /* 0 on a bad description */
+rtp_status rtp_norm_bwd(const rtp_norm_desc *d, const rtp_norm_grads *g, void *stream);
+
+/* One AdamW step over any number of tensors as one launch: the slots of ring
+ * stores (FlatParameter paragraph: every parameter of a unit in one flat slot;
+ * between rtp_ring_flush and rtp_ring_zero_grads), norms, a router's matrix.
+ *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
+ *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * g: the fp32 gradient, times *scale_dev where that is given (clipping).
+ * p: the fp32 master copy if there is one (the parameter is then its value,
+ * rounded to nearest), else the parameter itself, 16-bit ones rounded at random
+ * (below): rounded to nearest, a step smaller than half their spacing would be
+ * lost for good.
+ * Moments live in blocks of RTP_ADAMW_BLOCK elements, tensor after tensor, each
+ * tensor beginning a block (what a last block holds behind its tensor has no
+ * part in anything and may be overwritten).  RTP_MOMENTS_F32: fp32.  RTP_MOMENTS_8BIT:
+ * one byte an element and, for each block, one byte for m and one for v (exps [blocks, 2]):
+ * E, the biased fp32 exponent of the block's largest magnitude (at least 1).
+ *   m: sign, 4 bits of exponent e, 3 of fraction f: 2^(e - 14 + E - 127) (1 + f/8),
+ *   v: 5 bits of exponent, 3 of fraction:           2^(e - 30 + E - 127) (1 + f/8),
+ *   e = 0: 2^(1 - 14 + E - 127) f/8 (30 for v).  E = 255: the block holds
+ *   infinities or NaN and reads as NaN.
+ * They are rounded at random (up with the probability that makes the mean
+ * right): a moment moves by 1 - beta of itself a step, less than half a code's
+ * spacing, and would never move if rounded to nearest.  A second moment above
+ * zero is stored as code 1 at least.  The random bits are a hash of `seed` and
+ * the element's place in the moments: give another seed every step; the same
+ * one repeats the same bits. */
+#define RTP_ADAMW_BLOCK 256
+typedef enum { RTP_MOMENTS_F32 = 0, RTP_MOMENTS_8BIT = 1 } rtp_moments;
+typedef struct rtp_adamw rtp_adamw;
+typedef struct {
+    void *param_dev;
+    const float *grad_dev;
+    float *master_dev;    /* NULL: none; always NULL for RTP_F32 parameters       */
+    int64_t numel;        /* > 0                                                  */
+    rtp_dtype dtype;
+    float weight_decay;   /* finite                                               */
+} rtp_adamw_tensor;
+typedef struct {
+    const rtp_adamw_tensor *tensors; /* host; not looked at after create          */
+    int count;            /* 1 .. 2^20                                            */
+    rtp_moments moments;
+    void *m_dev, *v_dev;  /* rtp_adamw_blocks() * RTP_ADAMW_BLOCK fp32 or bytes, 16-byte aligned; zeros to begin with */
+    uint8_t *exps_dev;    /* RTP_MOMENTS_8BIT: [blocks, 2], 2-byte aligned; any value while the moments are zeros, but 255 */
+    void *table_dev;      /* rtp_adamw_table_bytes(), 16-byte aligned: the library's until destroy */
+    void *stream;         /* for writing the table; create waits for it           */
+} rtp_adamw_desc;
+int64_t rtp_adamw_blocks(const rtp_adamw_tensor *tensors, int count);     /* -1 for bad arguments */
+size_t rtp_adamw_table_bytes(const rtp_adamw_tensor *tensors, int count); /* 0 for bad arguments  */
+/* Errors: RTP_ERR_INVALID (null, bad enum, memory that is written and overlaps
+ * other memory of the step, the same tensor twice among it), RTP_ERR_SHAPE
+ * (sizes, alignment to elements), RTP_ERR_UNSUPPORTED (the stream is being captured). */
+rtp_status rtp_adamw_create(rtp_adamw **out, const rtp_adamw_desc *desc);
+rtp_status rtp_adamw_destroy(rtp_adamw *opt);
+
+typedef struct {
+    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps > 0                         */
+    int64_t step;                 /* 1 for the first                                */
+    uint32_t seed;
+} rtp_adamw_hyper;
+/* What the kernel needs of them.  A captured step replays with the values it
+ * was captured with, unless it was given scalars_dev: then it reads them from
+ * device memory (16-byte aligned), where the program puts the next step's before each replay. */
+typedef struct {
+    float beta1, one_minus_beta1, beta2, one_minus_beta2;
+    float lr, step_size, root_scale, eps; /* lr / (1 - beta1^step), 1 / sqrt(1 - beta2^step) */
+    uint32_t seed, reserved[3];
+} rtp_adamw_scalars;
+rtp_status rtp_adamw_scalars_of(const rtp_adamw_hyper *h, rtp_adamw_scalars *out); /* pure host */
+/* Exactly one of h and scalars_dev.  scale_dev: fp32 scalar or NULL; where it is not
+ * finite the step changes nothing (a gradient norm that overflowed). */
+rtp_status rtp_adamw_step(rtp_adamw *opt, const rtp_adamw_hyper *h, const rtp_adamw_scalars *scalars_dev,
+                          const float *scale_dev, void *stream);
+/* The moments as numbers, blocks * RTP_ADAMW_BLOCK each, fp32 or bf16 (8-bit
+ * moments are bf16 numbers exactly): checkpoints, inspection. */
+rtp_status rtp_adamw_moments(const rtp_adamw *opt, rtp_dtype dtype, void *m_out_dev, void *v_out_dev, void *stream);
+
 /* ---- single GEMM launch (kernel tests and roofline timing) -------------- */
 
 /* C[M,N] (+)= op(A) op(B) on `stream`, bf16 or f32 inputs, layout 0 NT

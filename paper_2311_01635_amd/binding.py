@@ -30,6 +30,15 @@ RTP_FLAG_PIPELINED = 8
 RTP_FLAG_STAGE_MEMCPY = 16
 RTP_FLAG_FUSED_STEP = 32
 RTP_NOALLOC_ACC_BYTES = 16 << 20
+RTP_SCORE_SOFTMAX, RTP_SCORE_SIGMOID = 0, 1
+RTP_ROUTE_MAX_EXPERTS, RTP_ROUTE_MAX_TOP, RTP_ROUTE_MAX_GROUPS, RTP_COMBINE_MAX_TOP = 1024, 32, 64, 32
+RTP_COMBINE_MAX_D = 1 << 20
+RTP_NORM_RMS, RTP_NORM_LAYER = 0, 1
+RTP_GATE_NONE, RTP_GATE_CHANNEL, RTP_GATE_ELEMENT = 0, 1, 2
+RTP_NORM_JOIN, RTP_NORM_POST, RTP_NORM_PRE = 1, 2, 4
+RTP_NORM_MAX_D = 1 << 20
+RTP_MOMENTS_F32, RTP_MOMENTS_8BIT = 0, 1
+RTP_ADAMW_BLOCK = 256
 LAYOUT_NT, LAYOUT_NN, LAYOUT_TN = 0, 1, 2
 
 TRACE_KINDS = {1: "fwd", 2: "bwd", 3: "w_in", 4: "w_out", 5: "g_in", 6: "g_out"}
@@ -72,6 +81,51 @@ class rtp_moe_desc(C.Structure):
                 ("yp_dev", C.c_void_p), ("dpre_dev", C.c_void_p), ("dxp_dev", C.c_void_p),
                 ("perm_dev", C.c_void_p), ("counts_dev", C.c_void_p),
                 ("compute_stream", C.c_void_p), ("stage_stream", C.c_void_p), ("aux_stream", C.c_void_p)]
+
+
+class rtp_route_desc(C.Structure):
+    _fields_ = [("T", C.c_int64), ("E", C.c_int), ("k", C.c_int), ("score", C.c_int), ("renormalise", C.c_int),
+                ("scale", C.c_float), ("groups", C.c_int), ("kept_groups", C.c_int), ("group_top", C.c_int),
+                ("dtype", C.c_int), ("grad_dtype", C.c_int), ("ld", C.c_int64), ("ld_grad", C.c_int64)]
+
+
+class rtp_norm_desc(C.Structure):
+    _fields_ = [("T", C.c_int64), ("D", C.c_int64), ("kind", C.c_int), ("parts", C.c_uint), ("gate", C.c_int),
+                ("stream_dtype", C.c_int), ("dtype", C.c_int), ("eps", C.c_float), ("res_scale", C.c_float),
+                ("out_scale", C.c_float), ("w_post_dev", C.c_void_p), ("b_post_dev", C.c_void_p),
+                ("w_pre_dev", C.c_void_p), ("b_pre_dev", C.c_void_p), ("gate_dev", C.c_void_p), ("ld_gate", C.c_int64)]
+
+
+class rtp_norm_io(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("x_dev", "y_dev", "r_dev", "h_dev", "stats_dev")] +
+                [(n, C.c_int64) for n in ("ld_x", "ld_y", "ld_r", "ld_h")])
+
+
+class rtp_norm_grads(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("r_dev", "y_dev", "dr_dev", "dh_dev", "stats_dev", "dx_dev", "dy_dev", "dgate_dev",
+                                           "dw_post_dev", "db_post_dev", "dw_pre_dev", "db_pre_dev")] +
+                [("accumulate", C.c_int), ("ws_dev", C.c_void_p), ("ws_bytes", C.c_size_t)] +
+                [(n, C.c_int64) for n in ("ld_r", "ld_y", "ld_dr", "ld_dh", "ld_dx", "ld_dy", "ld_dgate")])
+
+
+class rtp_adamw_tensor(C.Structure):
+    _fields_ = [("param_dev", C.c_void_p), ("grad_dev", C.c_void_p), ("master_dev", C.c_void_p), ("numel", C.c_int64),
+                ("dtype", C.c_int), ("weight_decay", C.c_float)]
+
+
+class rtp_adamw_desc(C.Structure):
+    _fields_ = [("tensors", C.POINTER(rtp_adamw_tensor)), ("count", C.c_int), ("moments", C.c_int), ("m_dev", C.c_void_p),
+                ("v_dev", C.c_void_p), ("exps_dev", C.c_void_p), ("table_dev", C.c_void_p), ("stream", C.c_void_p)]
+
+
+class rtp_adamw_hyper(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double),
+                ("step", C.c_int64), ("seed", C.c_uint32)]
+
+
+class rtp_adamw_scalars(C.Structure):
+    _fields_ = ([(n, C.c_float) for n in ("beta1", "one_minus_beta1", "beta2", "one_minus_beta2", "lr", "step_size",
+                                          "root_scale", "eps")] + [("seed", C.c_uint32), ("reserved", C.c_uint32 * 3)])
 
 
 class rtp_prof_result(C.Structure):
@@ -147,6 +201,20 @@ SYMBOLS = {
     "rtp_moe_set_ablation": (C.c_int, [_P, C.c_int, C.c_int]),
     "rtp_moe_sync": (C.c_int, [_P]),
     "rtp_moe_ring": (_P, [_P]),
+    "rtp_route_fwd": (C.c_int, [C.POINTER(rtp_route_desc), _P, _P, _P, _P, _P]),
+    "rtp_route_bwd": (C.c_int, [C.POINTER(rtp_route_desc), _P, _P, _P, _P, _P]),
+    "rtp_combine_fwd": (C.c_int, [C.c_int64, C.c_int, C.c_int64, C.c_int, _P, C.c_int64, _P, _P, C.c_int64, _P]),
+    "rtp_combine_bwd": (C.c_int, [C.c_int64, C.c_int, C.c_int64, C.c_int, _P, C.c_int64, _P, C.c_int64, _P, _P, C.c_int64, _P, _P]),
+    "rtp_norm_fwd": (C.c_int, [C.POINTER(rtp_norm_desc), C.POINTER(rtp_norm_io), _P]),
+    "rtp_norm_ws_bytes": (C.c_size_t, [C.POINTER(rtp_norm_desc)]),
+    "rtp_norm_bwd": (C.c_int, [C.POINTER(rtp_norm_desc), C.POINTER(rtp_norm_grads), _P]),
+    "rtp_adamw_blocks": (C.c_int64, [C.POINTER(rtp_adamw_tensor), C.c_int]),
+    "rtp_adamw_table_bytes": (C.c_size_t, [C.POINTER(rtp_adamw_tensor), C.c_int]),
+    "rtp_adamw_create": (C.c_int, [C.POINTER(_P), C.POINTER(rtp_adamw_desc)]),
+    "rtp_adamw_destroy": (C.c_int, [_P]),
+    "rtp_adamw_scalars_of": (C.c_int, [C.POINTER(rtp_adamw_hyper), C.POINTER(rtp_adamw_scalars)]),
+    "rtp_adamw_step": (C.c_int, [_P, C.POINTER(rtp_adamw_hyper), _P, _P, _P]),
+    "rtp_adamw_moments": (C.c_int, [_P, C.c_int, _P, _P, _P]),
     "rtp_gemm": (C.c_int, [C.c_int, C.c_int, C.c_int, C.c_int, _P, C.c_int64, _P, C.c_int64, _P, C.c_int64,
                            C.c_int64, C.c_int64, C.c_int64, C.c_int, _P]),
     "rtp_gemm_kernel_name": (C.c_char_p, [C.c_int, C.c_int]),

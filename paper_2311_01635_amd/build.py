@@ -12,7 +12,10 @@ SOURCES = ["rtp_gemm_pp_nt.hip", "rtp_gemm_pp_nn.hip", "rtp_gemm_pp_tn.hip",
            "rtp_gemm_pp_nt_f16.hip", "rtp_gemm_pp_nn_f16.hip", "rtp_gemm_pp_tn_f16.hip",
            "rtp_gemm_bf16.hip", "rtp_gemm_pp_nn_tn.hip", "rtp_gemm_pp_nn_tn_f16.hip",
            "rtp_gemm_duo_nt.hip", "rtp_gemm_duo_nn_tn.hip", "rtp_gemm_duo_nt_f16.hip", "rtp_gemm_duo_nn_tn_f16.hip",
-           "rtp_gemm_pp.hip", "rtp_misc_kernels.hip", "rtp_host.cpp"]
+           "rtp_gemm_pp.hip", "rtp_misc_kernels.hip", "rtp_norm.hip", "rtp_route.hip", "rtp_adamw.hip", "rtp_combine.hip",
+           "rtp_host.cpp", "rtp_block.cpp"]
+# the kernels of what stands around a unit (they share no header with the GEMMs)
+BLOCK_KERNELS = ("rtp_norm.hip", "rtp_route.hip", "rtp_adamw.hip", "rtp_combine.hip")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # -packed-fp32-ops off: the compiler must not form packed fp32 arithmetic from scalar code
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function",
@@ -26,12 +29,13 @@ def _newer(dst, srcs):
 def build(force: bool = True, verbose: bool = False) -> str:
     os.makedirs(OBJ, exist_ok=True)
     kernel_headers = [os.path.join(CSRC, h) for h in ("rtp_kernels.h", "rtp_ride.h", "rtp_gemm_epilogue.h", "rtp_gemm_pp.h", "rtp_gemm_small.h", "rtp_gemm_duo.h")]
-    host_headers = [os.path.join(CSRC, "rtp_kernels.h"), os.path.join(HERE, "..", "include", "rtp.h")]
+    block_headers = [os.path.join(CSRC, h) for h in ("rtp_elem.h", "rtp_block_kernels.h")] + [os.path.join(HERE, "..", "include", "rtp.h")]
+    host_headers = [os.path.join(CSRC, h) for h in ("rtp_kernels.h", "rtp_block_kernels.h", "rtp_error.h")] + [os.path.join(HERE, "..", "include", "rtp.h")]
 
     def compile_one(src):
         s = os.path.join(CSRC, src)
         o = os.path.join(OBJ, os.path.splitext(src)[0] + ".o")
-        headers = host_headers if src == "rtp_host.cpp" else kernel_headers
+        headers = host_headers if src.endswith(".cpp") else block_headers if src in BLOCK_KERNELS else kernel_headers
         if force or not _newer(o, [s] + headers):
             cmd = [HIPCC] + FLAGS + ["-c", s, "-o", o]
             tiled = src.startswith(("rtp_gemm_pp_", "rtp_gemm_duo_"))

@@ -3,6 +3,7 @@
 // the stage stream, and the per-step kernel launches.  No device memory is
 // allocated here; the only HIP objects owned are events.
 #include "../../include/rtp.h"
+#include "rtp_error.h"
 #include "rtp_kernels.h"
 
 #include <hip/hip_runtime.h>
@@ -23,7 +24,7 @@ using namespace rtp;
 // ---------------------------------------------------------------------------
 static thread_local char g_err[512] = "";
 
-static rtp_status fail(rtp_status s, const char *fmt, ...)
+rtp_status rtp::fail(rtp_status s, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -31,18 +32,6 @@ static rtp_status fail(rtp_status s, const char *fmt, ...)
     va_end(ap);
     return s;
 }
-
-#define HIP_TRY(expr)                                                                                       \
-    do {                                                                                                    \
-        hipError_t e_ = (expr);                                                                             \
-        if (e_ != hipSuccess) return fail(RTP_ERR_HIP, "%s: %s", #expr, hipGetErrorString(e_));             \
-    } while (0)
-
-#define RTP_TRY(expr)                       \
-    do {                                    \
-        rtp_status s_ = (expr);             \
-        if (s_ != RTP_OK) return s_;        \
-    } while (0)
 
 extern "C" const char *rtp_last_error(void) { return g_err; }
 

@@ -1,0 +1,281 @@
+// Norms before and after a unit with its gate and residual (rtp_norm_fwd, rtp_norm_bwd).
+#include "rtp_block_kernels.h"
+#include "rtp_elem.h"
+#include <algorithm>
+
+namespace rtp {
+
+constexpr int NT = 256, NW = NT / 64;
+
+// (a, b) summed over the workgroup, in every thread; `lds` is free again when it returns
+__device__ __forceinline__ float2 group_sum(float a, float b, float2 *lds)
+{
+    a = wave_sum(a);
+    b = wave_sum(b);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    float2 r = lds[0];
+    for (int i = 1; i < NW; ++i) r = make_float2(r.x + lds[i].x, r.y + lds[i].y);
+    __syncthreads();
+    return r;
+}
+
+struct NormFwd {
+    rtp_norm_desc d;
+    rtp_norm_io io;
+};
+
+// One workgroup a row, the row read once for each sum over it.
+template <rtp_dtype SD, rtp_dtype BD>
+__global__ __launch_bounds__(NT) void norm_fwd_row_kernel(NormFwd p)
+{
+    using S = typename Elem<SD>::t;
+    using B = typename Elem<BD>::t;
+    __shared__ float2 lds[NW];
+    const int64_t D = p.d.D;
+    const bool layer = p.d.kind == RTP_NORM_LAYER, join = p.d.parts & RTP_NORM_JOIN, post = p.d.parts & RTP_NORM_POST;
+    const float inv = 1.0f / (float)D;
+    for (int64_t row = blockIdx.x; row < p.d.T; row += gridDim.x) {
+        const S *x = (const S *)p.io.x_dev + row * p.io.ld_x;
+        const B *y = (const B *)p.io.y_dev + row * p.io.ld_y;
+        const S *v = x; // what the second norm is of
+        float mu = 0.0f, rs = 1.0f;
+        if (post) {
+            if (layer) {
+                float a = 0.0f;
+                for (int64_t i = threadIdx.x; i < D; i += NT) a += (float)y[i];
+                mu = group_sum(a, 0.0f, lds).x * inv;
+            }
+            float q = 0.0f;
+            for (int64_t i = threadIdx.x; i < D; i += NT) { const float c = (float)y[i] - mu; q += c * c; }
+            rs = 1.0f / sqrtf(group_sum(q, 0.0f, lds).x * inv + p.d.eps);
+            if (threadIdx.x == 0) { p.io.stats_dev[row * 4] = mu; p.io.stats_dev[row * 4 + 1] = rs; }
+        }
+        if (join) {
+            S *r = (S *)p.io.r_dev + row * p.io.ld_r;
+            for (int64_t i = threadIdx.x; i < D; i += NT) {
+                float o = (float)y[i];
+                if (post) {
+                    o = (o - mu) * rs;
+                    if (p.d.w_post_dev) o *= p.d.w_post_dev[i];
+                    if (p.d.b_post_dev) o += p.d.b_post_dev[i];
+                }
+                if (p.d.gate == RTP_GATE_CHANNEL) o *= ((const float *)p.d.gate_dev)[i];
+                if (p.d.gate == RTP_GATE_ELEMENT) o *= (float)((const B *)p.d.gate_dev)[row * p.d.ld_gate + i];
+                r[i] = (S)(p.d.res_scale * (float)x[i] + p.d.out_scale * o);
+            }
+            v = r; // (every thread reads back what it wrote itself)
+        }
+        if (p.d.parts & RTP_NORM_PRE) {
+            B *h = (B *)p.io.h_dev + row * p.io.ld_h;
+            mu = 0.0f;
+            if (layer) {
+                float a = 0.0f;
+                for (int64_t i = threadIdx.x; i < D; i += NT) a += (float)v[i];
+                mu = group_sum(a, 0.0f, lds).x * inv;
+            }
+            float q = 0.0f;
+            for (int64_t i = threadIdx.x; i < D; i += NT) { const float c = (float)v[i] - mu; q += c * c; }
+            rs = 1.0f / sqrtf(group_sum(q, 0.0f, lds).x * inv + p.d.eps);
+            if (threadIdx.x == 0) { p.io.stats_dev[row * 4 + 2] = mu; p.io.stats_dev[row * 4 + 3] = rs; }
+            for (int64_t i = threadIdx.x; i < D; i += NT) {
+                float o = ((float)v[i] - mu) * rs;
+                if (p.d.w_pre_dev) o *= p.d.w_pre_dev[i];
+                if (p.d.b_pre_dev) o += p.d.b_pre_dev[i];
+                h[i] = (B)o;
+            }
+        }
+    }
+}
+
+struct NormBwd {
+    rtp_norm_desc d;
+    rtp_norm_grads g;
+    unsigned sums;
+    int nsums;
+};
+
+// A workgroup takes every gridDim.x-th row and keeps its column sums in its own part of the workspace, where each column is
+// one thread's.
+template <rtp_dtype SD, rtp_dtype BD>
+__global__ __launch_bounds__(NT) void norm_bwd_row_kernel(NormBwd p)
+{
+    using S = typename Elem<SD>::t;
+    using B = typename Elem<BD>::t;
+    __shared__ float2 lds[NW];
+    const int64_t D = p.d.D;
+    const bool layer = p.d.kind == RTP_NORM_LAYER, join = p.d.parts & RTP_NORM_JOIN, post = p.d.parts & RTP_NORM_POST, pre = p.d.parts & RTP_NORM_PRE;
+    const float inv = 1.0f / (float)D;
+    float *ws = (float *)p.g.ws_dev + (int64_t)blockIdx.x * p.nsums * D;
+    for (int64_t i = threadIdx.x; i < p.nsums * D; i += NT) ws[i] = 0.0f;
+    __syncthreads();
+    for (int64_t row = blockIdx.x; row < p.d.T; row += gridDim.x) {
+        const S *r = (const S *)p.g.r_dev + row * p.g.ld_r, *dr = p.g.dr_dev ? (const S *)p.g.dr_dev + row * p.g.ld_dr : nullptr;
+        const B *y = (const B *)p.g.y_dev + row * p.g.ld_y, *dh = (const B *)p.g.dh_dev + row * p.g.ld_dh;
+        const B *gate = (const B *)p.d.gate_dev + row * p.d.ld_gate;
+        S *dx = (S *)p.g.dx_dev + row * p.g.ld_dx;
+        B *dy = (B *)p.g.dy_dev + row * p.g.ld_dy;
+        float4 st = {0.0f, 1.0f, 0.0f, 1.0f};
+        if (post) { st.x = p.g.stats_dev[row * 4]; st.y = p.g.stats_dev[row * 4 + 1]; }
+        if (pre) { st.z = p.g.stats_dev[row * 4 + 2]; st.w = p.g.stats_dev[row * 4 + 3]; }
+        float2 m1 = {0.0f, 0.0f}, m2 = {0.0f, 0.0f};
+        if (pre) {
+            float a = 0.0f, b = 0.0f;
+            for (int64_t i = threadIdx.x; i < D; i += NT) {
+                const float dn = (float)dh[i] * (p.d.w_pre_dev ? p.d.w_pre_dev[i] : 1.0f);
+                a += dn;
+                b += dn * ((float)r[i] - st.z) * st.w;
+            }
+            m1 = group_sum(a, b, lds);
+            m1 = {layer ? m1.x * inv : 0.0f, m1.y * inv};
+        }
+        // gradient of the stream's row at i
+        auto stream = [&](int64_t i) {
+            float v = dr ? (float)dr[i] : 0.0f;
+            if (pre) {
+                const float dn = (float)dh[i] * (p.d.w_pre_dev ? p.d.w_pre_dev[i] : 1.0f);
+                v += st.w * (dn - m1.x - ((float)r[i] - st.z) * st.w * m1.y);
+            }
+            return v;
+        };
+        // ... of gate . N(y), with the gate's factor
+        auto branch = [&](int64_t i, float v) {
+            v *= p.d.out_scale;
+            if (p.d.gate == RTP_GATE_CHANNEL) v *= ((const float *)p.d.gate_dev)[i];
+            if (p.d.gate == RTP_GATE_ELEMENT) v *= (float)gate[i];
+            return v;
+        };
+        if (post) {
+            float a = 0.0f, b = 0.0f;
+            for (int64_t i = threadIdx.x; i < D; i += NT) {
+                const float dn = branch(i, stream(i)) * (p.d.w_post_dev ? p.d.w_post_dev[i] : 1.0f);
+                a += dn;
+                b += dn * ((float)y[i] - st.x) * st.y;
+            }
+            m2 = group_sum(a, b, lds);
+            m2 = {layer ? m2.x * inv : 0.0f, m2.y * inv};
+        }
+        for (int64_t i = threadIdx.x; i < D; i += NT) {
+            const float v = stream(i);
+            float *w = ws + i;
+            if (p.sums & SUM_PRE_W) { *w += (float)dh[i] * ((float)r[i] - st.z) * st.w; w += D; }
+            if (p.sums & SUM_PRE_B) { *w += (float)dh[i]; w += D; }
+            dx[i] = (S)((join ? p.d.res_scale : 1.0f) * v);   // (dx may be dr: its last reader has read it)
+            if (!join) continue;
+            const bool has_y = post || p.d.gate != RTP_GATE_NONE;
+            const float n = has_y ? ((float)y[i] - st.x) * st.y : 0.0f, wp = post && p.d.w_post_dev ? p.d.w_post_dev[i] : 1.0f;
+            const float e = branch(i, v), f = p.d.gate == RTP_GATE_CHANNEL ? p.d.out_scale * v : e;
+            if (p.sums & SUM_POST_W) { *w += f * n; w += D; }
+            if (p.sums & SUM_POST_B) *w += f;
+            if (p.d.gate == RTP_GATE_ELEMENT && p.g.dgate_dev)
+                ((B *)p.g.dgate_dev)[row * p.g.ld_dgate + i] =
+                    (B)(p.d.out_scale * v * (n * wp + (post && p.d.b_post_dev ? p.d.b_post_dev[i] : 0.0f)));
+            dy[i] = (B)(post ? st.y * (e * wp - m2.x - n * m2.y) : e);
+        }
+    }
+}
+
+struct NormSums {
+    const float *ws;
+    int parts, nsums;
+    unsigned sums;
+    int64_t D;
+    float *dw_pre, *db_pre, *dw_post, *db_post, *dgate;
+    const float *gate, *w_post, *b_post; // of a channel gate
+    int accumulate;
+};
+
+// The parts' column sums, in order, and the gradients that follow from them: with a channel gate the sums over rows leave it
+// out, S = sum of b dR n and Q = sum of b dR, so that dw = gate S, db = gate Q, dgate = w S + b Q.
+__global__ __launch_bounds__(NT) void norm_sums_kernel(NormSums p)
+{
+    const int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x;
+    if (i >= p.D) return;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    int at = 0;
+    for (int k = 0; k < 4; ++k) {
+        if (!(p.sums >> k & 1)) continue;
+        for (int b = 0; b < p.parts; ++b) v[k] += p.ws[((int64_t)b * p.nsums + at) * p.D + i];
+        ++at;
+    }
+    auto put = [&](float *to, float x) {
+        if (to) to[i] = p.accumulate ? to[i] + x : x;
+    };
+    put(p.dw_pre, v[0]);
+    put(p.db_pre, v[1]);
+    const float gate = p.gate ? p.gate[i] : 1.0f;
+    put(p.dw_post, gate * v[2]);
+    put(p.db_post, gate * v[3]);
+    put(p.dgate, (p.w_post ? p.w_post[i] : 1.0f) * v[2] + (p.b_post ? p.b_post[i] * v[3] : 0.0f));
+}
+
+template <class F>
+static hipError_t by_types(const rtp_norm_desc &d, F f)
+{
+    if (d.stream_dtype == RTP_F32) {
+        if (d.dtype == RTP_F32) return f.template operator()<RTP_F32, RTP_F32>();
+        if (d.dtype == RTP_BF16) return f.template operator()<RTP_F32, RTP_BF16>();
+        return f.template operator()<RTP_F32, RTP_F16>();
+    }
+    if (d.dtype == RTP_BF16) return f.template operator()<RTP_BF16, RTP_BF16>();
+    return f.template operator()<RTP_F16, RTP_F16>();
+}
+
+struct RunFwd {
+    const NormFwd &p;
+    hipStream_t s;
+    template <rtp_dtype SD, rtp_dtype BD> hipError_t operator()()
+    {
+        norm_fwd_row_kernel<SD, BD><<<(unsigned)std::min<int64_t>(p.d.T, 1 << 20), NT, 0, s>>>(p);
+        return hipGetLastError();
+    }
+};
+
+hipError_t launch_norm_fwd(const rtp_norm_desc &d, const rtp_norm_io &io, hipStream_t s)
+{
+    const NormFwd p{d, io};
+    return by_types(d, RunFwd{p, s});
+}
+
+int norm_bwd_parts(const rtp_norm_desc &d) { return (int)std::min<int64_t>(d.T, 1024); }
+
+struct RunBwd {
+    const NormBwd &p;
+    hipStream_t s;
+    template <rtp_dtype SD, rtp_dtype BD> hipError_t operator()()
+    {
+        norm_bwd_row_kernel<SD, BD><<<norm_bwd_parts(p.d), NT, 0, s>>>(p);
+        return hipGetLastError();
+    }
+};
+
+hipError_t launch_norm_bwd(const rtp_norm_desc &d, const rtp_norm_grads &g, unsigned sums, hipStream_t s)
+{
+    const NormBwd p{d, g, sums, __builtin_popcount(sums)};
+    if (d.T > 0) {
+        const hipError_t e = by_types(d, RunBwd{p, s});
+        if (e != hipSuccess) return e;
+    }
+    if (!sums) return hipSuccess;
+    NormSums q{};
+    q.ws = (const float *)g.ws_dev;
+    q.parts = norm_bwd_parts(d);
+    q.nsums = p.nsums;
+    q.sums = sums;
+    q.D = d.D;
+    q.dw_pre = g.dw_pre_dev;
+    q.db_pre = g.db_pre_dev;
+    q.dw_post = g.dw_post_dev;
+    q.db_post = g.db_post_dev;
+    if (d.gate == RTP_GATE_CHANNEL) {
+        q.dgate = (float *)g.dgate_dev;
+        q.gate = (const float *)d.gate_dev;
+    }
+    q.w_post = d.parts & RTP_NORM_POST ? d.w_post_dev : nullptr;
+    q.b_post = d.parts & RTP_NORM_POST ? d.b_post_dev : nullptr;
+    q.accumulate = g.accumulate;
+    norm_sums_kernel<<<(unsigned)((d.D + NT - 1) / NT), NT, 0, s>>>(q);
+    return hipGetLastError();
+}
+
+} // namespace rtp

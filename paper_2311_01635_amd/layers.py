@@ -6,6 +6,7 @@ import ctypes as C
 import torch
 
 from . import binding as B
+from .block import RtpCombine
 
 _TORCH_DT = {B.RTP_F32: torch.float32, B.RTP_BF16: torch.bfloat16, B.RTP_F16: torch.float16}
 
@@ -143,6 +144,9 @@ class RtpLinear(_PassStreams):
         torch.cuda.synchronize(self.dev)
         return out
 
+    def ring_handle(self):
+        return self.ring.handle
+
     def gathered_bias(self):
         """(b, gradient of b) read back from the home store (call gathered() first: it flushes)."""
         out = self.store_w.unpack("b"), self.store_g.unpack("b")
@@ -262,6 +266,9 @@ class RtpMlp(_PassStreams):
         torch.cuda.synchronize(self.dev)
         return out
 
+    def ring_handle(self):
+        return B.lib.rtp_mlp_ring(self.handle)
+
     def gathered_biases(self):
         """(biases, their gradients), each in the order the matrices were given, from the home store (call
         gathered() first: it flushes)."""
@@ -277,14 +284,20 @@ class RtpMlp(_PassStreams):
 
 class RtpMoe(_PassStreams):
     """Expert-partitioned layer run by rtp_moe_fwd / rtp_moe_bwd: the ring's
-    shard is one whole expert.  `experts[e]` = (W1, W2) or (Wg, Wu, Wd)."""
+    shard is one whole expert.  `experts[e]` = (W1, W2) or (Wg, Wu, Wd).
+
+    top_k > 1, or weights in the calls: a token goes to top_k experts (`route` is RtpRouter's ids [T, top_k]) and its output is
+    their weighted sum.  The layer below then works on T * top_k rows, and backward() also gives the weights' gradient."""
 
     def __init__(self, experts, T, rank, act, mode=B.RTP_INPLACE_STAGED, dtype=B.RTP_BF16, G0=None,
-                 device="cuda:0", aux_stream=True):
+                 device="cuda:0", aux_stream=True, top_k=1):
         self.dev = torch.device(device)
         td = _TORCH_DT[dtype]
         n = len(experts)
-        self.n, self.rank, self.T, self.act, self.mode, self.dtype = n, rank, T, act, mode, dtype
+        self.n, self.rank, self.act, self.mode, self.dtype = n, rank, act, mode, dtype
+        self.tokens, self.combine = T, RtpCombine(top_k)
+        self.xk = self.yk = self.gk = None         # rows of the slots, made when a weighted call needs them
+        T = self.T = T * top_k
         self.gated = act == B.RTP_ACT_SWIGLU
         self.shapes = [tuple(w.shape) for w in experts[0]]
         self.O, self.I = self.shapes[0]
@@ -341,15 +354,52 @@ class RtpMoe(_PassStreams):
         torch.cuda.synchronize(self.dev)
         B.check(B.lib.rtp_moe_create(C.byref(self.handle), C.byref(d)), "rtp_moe_create")
 
-    def forward(self, X, route, Y):
+    def forward(self, X, route, Y, weights=None):
+        k = self.combine.k
+        if k == 1 and weights is None:
+            self._forward(X, route, Y)
+            return
+        if tuple(route.shape) != (self.tokens, k) or route.dtype != torch.int32 or not route.is_contiguous():
+            raise ValueError(f"route must be a contiguous [{self.tokens}, {k}] tensor of int32")
+        self.yk = self._slots(self.yk, self.O2)
+        if k > 1:
+            self.xk = self._slots(self.xk, self.I)
+            self.combine.expand(X, self.xk)
+        self._forward(self.xk if k > 1 else X, route, self.yk)
+        self.combine.forward(self.yk, weights, Y)
+
+    def backward(self, dY, dX, weights=None, dweights=None):
+        """weights: those of forward().  dweights (fp32 [T, top_k], or None): their gradient."""
+        k = self.combine.k
+        if k == 1 and weights is None and dweights is None:
+            self._backward(dY, dX)
+            return
+        if dweights is not None and self.yk is None:
+            raise ValueError("the forward pass had no weights")
+        self.gk = self._slots(self.gk, self.O2)
+        self.combine.backward(dY, self.yk if dweights is not None else None, weights, self.gk, dweights)
+        if k == 1:
+            self._backward(self.gk, dX)
+            return
+        self.xk = self._slots(self.xk, self.I)      # (the layer keeps its own grouped copy of the forward pass's rows)
+        self._backward(self.gk, self.xk)
+        self.combine.forward(self.xk, None, dX)
+
+    def _slots(self, buf, cols):
+        return torch.empty(self.T, cols, dtype=_TORCH_DT[self.dtype], device=self.dev) if buf is None else buf
+
+    def _forward(self, X, route, Y):
         self._enter()
         B.check(B.lib.rtp_moe_fwd(self.handle, B._ptr(X), B._ptr(route), B._ptr(Y)), "rtp_moe_fwd")
         self._leave()
 
-    def backward(self, dY, dX):
+    def _backward(self, dY, dX):
         self._enter()
         B.check(B.lib.rtp_moe_bwd(self.handle, B._ptr(dY), B._ptr(dX)), "rtp_moe_bwd")
         self._leave()
+
+    def ring_handle(self):
+        return B.lib.rtp_moe_ring(self.handle)
 
     def sync(self):
         B.check(B.lib.rtp_moe_sync(self.handle), "rtp_moe_sync")
