@@ -266,6 +266,8 @@ rtp_status rtp_ring_abort(rtp_ring *ring);
  * store sees every shard (tests, checkpoints, an optimizer): between passes
  * the worker's copy is the only current one of the shard it holds (Memory
  * Arrangement section: each parameter exists once in the system).  Idle state only.
+ * The weights are copied by the first flush after a pass alone: the caller may
+ * have written the store since, and a later flush leaves it as it is.
  * Between a backward pass and the flush the home slot of the worker's own
  * gradient shard is stale: write to the gradient store only after a flush (or
  * through rtp_ring_zero_grads), else the next backward pass writes the

@@ -230,6 +230,7 @@ struct rtp_ring {
     bool pass_uses_as = true; // the open pass enqueues on the auxiliary stream (a schedule that does not says so)
     bool w_held = false; // buf_w[res_idx] really holds shard `resident` as the store has it (not after a flush,
                          // an abort, or a pass run with the rotation switched off)
+    bool w_flushed = false; // a flush has copied those weights home, and no pass has begun since
     int res_g = -1;      // shard whose gradients are in buf_g[res_g_idx]
     int res_g_idx = 0;
     int base_idx = 0;    // weight buffer index at step 0 of the open pass
@@ -696,6 +697,7 @@ extern "C" rtp_status rtp_ring_begin(rtp_ring *r, rtp_pass pass)
     RTP_TRY(begin_join(r));
     r->joined = r->rode = r->carry;
     r->pass = pass;
+    r->w_flushed = false;
     r->rotations = 0;
     r->executed = 0;
     for (rtp_linear *l : r->linears) {
@@ -772,6 +774,7 @@ extern "C" rtp_status rtp_ring_seek_bwd_start(rtp_ring *r)
     const int k = (r->d.rank + 1) % r->d.n;
     r->res_idx = 0;
     r->resident = k;
+    r->w_flushed = false;
     RTP_TRY(copy_async(r, r->d.buf_w_dev[0], r->home_w(k), r->d.w_bytes, r->cs()));
     r->rec(TR_W_IN, -1, k, 0);
     r->w_held = r->abl_rotate;
@@ -988,9 +991,12 @@ extern "C" rtp_status rtp_ring_flush(rtp_ring *r)
     RTP_TRY(ensure_events(r));
     RTP_TRY(idle_join(r));
     CopyBatch b;
-    RTP_TRY(copy_batch_add(r, b, r->home_w(r->resident), r->d.buf_w_dev[r->res_idx], r->d.w_bytes, r->cs()));
-    r->rec(TR_W_OUT, -1, r->resident, r->res_idx);
+    if (!r->w_flushed) { // (a second flush would put the old weights over what the caller has written since the first)
+        RTP_TRY(copy_batch_add(r, b, r->home_w(r->resident), r->d.buf_w_dev[r->res_idx], r->d.w_bytes, r->cs()));
+        r->rec(TR_W_OUT, -1, r->resident, r->res_idx);
+    }
     r->w_held = false; // the store may be written from here on (an optimizer step): the next forward pass loads anew
+    r->w_flushed = true;
     const bool held_g = r->d.g_bytes && r->res_g >= 0;
     if (held_g) RTP_TRY(copy_batch_add(r, b, r->home_g(r->res_g), r->d.buf_g_dev[r->res_g_idx], r->d.g_bytes, r->cs()));
     RTP_TRY(copy_batch_flush(r, b, r->cs()));
