@@ -220,8 +220,9 @@ def _own_combine(rtp, s):
 
 
 def _own_adamw(rtp, s):
-    tensors = [dict(param=s["w"][a:a + n], grad=s["g"][a:a + n], master=s["master"][a:a + n] if "master" in s else None, weight_decay=wd)
-               for a, n, wd in s["spans"]]
+    # a flat store of whole blocks: what fills up a tensor's last block is stepped with it, as in the plain form
+    whole = [(slice(a, a - (-n // BLOCK) * BLOCK), wd) for a, n, wd in s["spans"]]
+    tensors = [dict(param=s["w"][a], grad=s["g"][a], master=s["master"][a] if "master" in s else None, weight_decay=wd) for a, wd in whole]
     s["opt"] = rtp.RtpAdamW(tensors, state=s["case"]["state"], moments=(s["m"], s["v"], s.get("exps")))
 
 
