@@ -1,4 +1,4 @@
-// Element types of the kernels around a unit, and what their rows are read and written with.
+// Element types of the kernels around a unit, and how their rows are read and written.
 #pragma once
 #include "../../include/rtp.h"
 #include <hip/hip_runtime.h>
@@ -9,6 +9,70 @@ template <rtp_dtype D> struct Elem;
 template <> struct Elem<RTP_F32> { using t = float; };
 template <> struct Elem<RTP_BF16> { using t = __bf16; };
 template <> struct Elem<RTP_F16> { using t = _Float16; };
+
+// Eight neighbouring elements as they are in memory.  Rows may begin anywhere (an odd length, a column of a wider matrix): the
+// hardware reads and writes 16 bytes at any address of an element, and a row that begins off 16 bytes costs the lines it
+// touches, no path of its own.  What is left of a row behind its last whole eight goes element by element (`n` of them).
+template <rtp_dtype D> struct Eight {
+    using t = typename Elem<D>::t;
+    static constexpr int WORDS = sizeof(t) * 2;
+    typedef uint32_t Raw __attribute__((ext_vector_type(WORDS), aligned(sizeof(t))));
+    struct { uint32_t w[WORDS]; } raw;
+
+    __device__ __forceinline__ void load(const t *p, int64_t n)
+    {
+        if (n >= 8) {
+            const Raw v = *(const Raw *)p;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) raw.w[i] = v[i];
+        } else {
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) raw.w[i] = 0;
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (i < n) {
+                    if (sizeof(t) == 4) raw.w[i % WORDS] = ((const uint32_t *)p)[i];
+                    else raw.w[i / 2] |= (uint32_t)((const uint16_t *)p)[i] << (i & 1) * 16;
+                }
+        }
+    }
+    __device__ __forceinline__ void store(t *p, int64_t n) const
+    {
+        if (n >= 8) {
+            Raw v;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) v[i] = raw.w[i];
+            __builtin_nontemporal_store(v, (Raw *)p);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 7; ++i)
+                if (i < n) {
+                    if (sizeof(t) == 4) ((uint32_t *)p)[i] = raw.w[i % WORDS];
+                    else ((uint16_t *)p)[i] = (uint16_t)(raw.w[i / 2] >> (i & 1) * 16);
+                }
+        }
+    }
+    __device__ __forceinline__ float get(int i) const
+    {
+        if constexpr (D == RTP_F32) return __uint_as_float(raw.w[i % WORDS]);
+        const uint32_t h = raw.w[i / 2];
+        if (D == RTP_BF16) return __uint_as_float(i & 1 ? h & 0xFFFF0000u : h << 16);
+        return (float)__builtin_bit_cast(_Float16, (uint16_t)(i & 1 ? h >> 16 : h));
+    }
+    // (rounded to nearest, once)
+    __device__ __forceinline__ void set(const float (&v)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) {
+            if constexpr (D == RTP_F32) {
+                raw.w[i] = __float_as_uint(v[i % 8]);
+            } else {
+                const uint32_t lo = __builtin_bit_cast(uint16_t, (t)v[2 * i % 8]), hi = __builtin_bit_cast(uint16_t, (t)v[(2 * i + 1) % 8]);
+                raw.w[i] = lo | hi << 16;
+            }
+        }
+    }
+};
 
 // sum over the wave, in every lane
 __device__ __forceinline__ float wave_sum(float v)

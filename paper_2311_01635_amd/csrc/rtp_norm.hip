@@ -5,17 +5,21 @@
 
 namespace rtp {
 
-constexpr int NT = 256, NW = NT / 64;
+constexpr int NT = 256;
 
-// (a, b) summed over the workgroup, in every thread; `lds` is free again when it returns
+// (a, b) summed over a group of `waves` waves that is the workgroup, or over a single wave; in every thread.  `lds` is free again
+// when it returns.
+template <int WAVES>
 __device__ __forceinline__ float2 group_sum(float a, float b, float2 *lds)
 {
     a = wave_sum(a);
     b = wave_sum(b);
+    if (WAVES == 1) return make_float2(a, b);
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(a, b);
     __syncthreads();
     float2 r = lds[0];
-    for (int i = 1; i < NW; ++i) r = make_float2(r.x + lds[i].x, r.y + lds[i].y);
+#pragma unroll
+    for (int i = 1; i < WAVES; ++i) r = make_float2(r.x + lds[i].x, r.y + lds[i].y);
     __syncthreads();
     return r;
 }
@@ -25,13 +29,163 @@ struct NormFwd {
     rtp_norm_io io;
 };
 
+// ---- rows that are held in registers ------------------------------------------------------------------------
+// Bound: HBM (a norm is 10 to 30 operations an element).  THREADS threads share a row, NV times eight elements each, which are
+// read once and stay in registers over the sums; a wave alone needs no barrier.  A workgroup goes on to other rows so that the
+// parameters, which would otherwise come out of L2 as often as the rows out of HBM, are fetched once.
+
+template <int THREADS> constexpr int norm_block() { return THREADS < 256 ? 256 : THREADS; }
+
+__device__ __forceinline__ void load_params(float (&v)[8], const float *p, int64_t i, int64_t n, float missing)
+{
+    Eight<RTP_F32> e;
+    if (p) e.load(p + i, n);
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = p ? e.get(k) : missing;
+}
+
+template <rtp_dtype SD, rtp_dtype BD, int THREADS, int NV, bool BIAS>
+__global__ __launch_bounds__(norm_block<THREADS>()) void norm_fwd_kernel(NormFwd p)
+{
+    using S = typename Elem<SD>::t;
+    using B = typename Elem<BD>::t;
+    constexpr int WAVES = THREADS / 64, ROWS = norm_block<THREADS>() / THREADS;
+    // 1024 threads have 128 registers each: no room for parameters and another row beside the present one
+    constexpr bool KEEP = THREADS < 1024;
+    __shared__ float2 lds[WAVES];
+    const int tid = threadIdx.x % THREADS;
+    const int64_t D = p.d.D;
+    const bool layer = p.d.kind == RTP_NORM_LAYER, join = p.d.parts & RTP_NORM_JOIN, post = p.d.parts & RTP_NORM_POST, pre = p.d.parts & RTP_NORM_PRE;
+    const bool elem = p.d.gate == RTP_GATE_ELEMENT;
+    const float inv = 1.0f / (float)D;
+    // r = res_scale x + (n a + c) g with a = out_scale gate w_post, c = out_scale gate b_post
+    int64_t at[NV], left[NV];
+    float a[NV][8], c[NV][8], w[NV][8], b[NV][8];
+    auto post_params = [&](int j) {
+        float g[8];
+        load_params(a[j], p.d.w_post_dev, at[j], left[j], 1.0f);
+        load_params(g, p.d.gate == RTP_GATE_CHANNEL ? (const float *)p.d.gate_dev : nullptr, at[j], left[j], 1.0f);
+        if (BIAS) load_params(c[j], p.d.b_post_dev, at[j], left[j], 0.0f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            g[k] *= p.d.out_scale;
+            a[j][k] *= g[k];
+            if (BIAS) c[j][k] *= g[k];
+        }
+    };
+    auto pre_params = [&](int j) {
+        load_params(w[j], p.d.w_pre_dev, at[j], left[j], 1.0f);
+        if (BIAS) load_params(b[j], p.d.b_pre_dev, at[j], left[j], 0.0f);
+    };
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        at[j] = (tid + j * THREADS) * 8;
+        left[j] = D - at[j];
+        if (KEEP) {
+            post_params(j);
+            pre_params(j);
+        }
+    }
+    // mean and 1 / deviation of a row in registers
+    auto moments = [&](const float (&v)[NV][8], float &mu, float &rs) {
+        mu = 0.0f;
+        if (layer) {
+            float s = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) s += v[j][k];
+            mu = group_sum<WAVES>(s, 0.0f, lds).x * inv;
+        }
+        float q = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float x = k < left[j] ? v[j][k] - mu : 0.0f;
+                q += x * x;
+            }
+        rs = 1.0f / sqrtf(group_sum<WAVES>(q, 0.0f, lds).x * inv + p.d.eps);
+    };
+    const int64_t stride = (int64_t)gridDim.x * ROWS;
+    int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS;
+    Eight<SD> x[NV], next_x[NV];
+    Eight<BD> y[NV], g[NV], next_y[NV], next_g[NV];
+    auto fetch = [&](int64_t r) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (left[j] <= 0) continue;
+            next_x[j].load((const S *)p.io.x_dev + r * p.io.ld_x + at[j], left[j]);
+            if (join) next_y[j].load((const B *)p.io.y_dev + r * p.io.ld_y + at[j], left[j]);
+            if (elem) next_g[j].load((const B *)p.d.gate_dev + r * p.d.ld_gate + at[j], left[j]);
+        }
+    };
+    if (row < p.d.T) fetch(row);
+    for (; row < p.d.T; row += stride) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) { x[j] = next_x[j]; y[j] = next_y[j]; g[j] = next_g[j]; }
+        if (KEEP && row + stride < p.d.T) fetch(row + stride); // under this row's sums
+        float v[NV][8];
+        float mu = 0.0f, rs = 1.0f;
+        if (join) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[j][k] = left[j] > 0 ? y[j].get(k) : 0.0f;
+            if (post) {
+                moments(v, mu, rs);
+                if (tid == 0) { p.io.stats_dev[row * 4] = mu; p.io.stats_dev[row * 4 + 1] = rs; }
+            }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (left[j] <= 0) continue;
+                if (!KEEP) post_params(j);
+                float o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    o[k] = (v[j][k] - mu) * rs * a[j][k];
+                    if (BIAS) o[k] += c[j][k];
+                    if (elem) o[k] *= g[j].get(k);
+                    o[k] = p.d.res_scale * x[j].get(k) + o[k];
+                }
+                x[j].set(o);
+                x[j].store((S *)p.io.r_dev + row * p.io.ld_r + at[j], left[j]);
+            }
+        }
+        if (pre) { // (of the stream as it is stored)
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) v[j][k] = k < left[j] ? x[j].get(k) : 0.0f;
+            moments(v, mu, rs);
+            if (tid == 0) { p.io.stats_dev[row * 4 + 2] = mu; p.io.stats_dev[row * 4 + 3] = rs; }
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (left[j] <= 0) continue;
+                if (!KEEP) pre_params(j);
+                float o[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    o[k] = (v[j][k] - mu) * rs * w[j][k];
+                    if (BIAS) o[k] += b[j][k];
+                }
+                Eight<BD> h;
+                h.set(o);
+                h.store((B *)p.io.h_dev + row * p.io.ld_h + at[j], left[j]);
+            }
+        }
+        if (!KEEP && row + stride < p.d.T) fetch(row + stride);
+    }
+}
+
+// ---- rows of any length -------------------------------------------------------------------------------------
 // One workgroup a row, the row read once for each sum over it.
 template <rtp_dtype SD, rtp_dtype BD>
 __global__ __launch_bounds__(NT) void norm_fwd_row_kernel(NormFwd p)
 {
     using S = typename Elem<SD>::t;
     using B = typename Elem<BD>::t;
-    __shared__ float2 lds[NW];
+    __shared__ float2 lds[NT / 64];
     const int64_t D = p.d.D;
     const bool layer = p.d.kind == RTP_NORM_LAYER, join = p.d.parts & RTP_NORM_JOIN, post = p.d.parts & RTP_NORM_POST;
     const float inv = 1.0f / (float)D;
@@ -44,11 +198,11 @@ __global__ __launch_bounds__(NT) void norm_fwd_row_kernel(NormFwd p)
             if (layer) {
                 float a = 0.0f;
                 for (int64_t i = threadIdx.x; i < D; i += NT) a += (float)y[i];
-                mu = group_sum(a, 0.0f, lds).x * inv;
+                mu = group_sum<NT / 64>(a, 0.0f, lds).x * inv;
             }
             float q = 0.0f;
             for (int64_t i = threadIdx.x; i < D; i += NT) { const float c = (float)y[i] - mu; q += c * c; }
-            rs = 1.0f / sqrtf(group_sum(q, 0.0f, lds).x * inv + p.d.eps);
+            rs = 1.0f / sqrtf(group_sum<NT / 64>(q, 0.0f, lds).x * inv + p.d.eps);
             if (threadIdx.x == 0) { p.io.stats_dev[row * 4] = mu; p.io.stats_dev[row * 4 + 1] = rs; }
         }
         if (join) {
@@ -72,11 +226,11 @@ __global__ __launch_bounds__(NT) void norm_fwd_row_kernel(NormFwd p)
             if (layer) {
                 float a = 0.0f;
                 for (int64_t i = threadIdx.x; i < D; i += NT) a += (float)v[i];
-                mu = group_sum(a, 0.0f, lds).x * inv;
+                mu = group_sum<NT / 64>(a, 0.0f, lds).x * inv;
             }
             float q = 0.0f;
             for (int64_t i = threadIdx.x; i < D; i += NT) { const float c = (float)v[i] - mu; q += c * c; }
-            rs = 1.0f / sqrtf(group_sum(q, 0.0f, lds).x * inv + p.d.eps);
+            rs = 1.0f / sqrtf(group_sum<NT / 64>(q, 0.0f, lds).x * inv + p.d.eps);
             if (threadIdx.x == 0) { p.io.stats_dev[row * 4 + 2] = mu; p.io.stats_dev[row * 4 + 3] = rs; }
             for (int64_t i = threadIdx.x; i < D; i += NT) {
                 float o = ((float)v[i] - mu) * rs;
@@ -102,7 +256,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_row_kernel(NormBwd p)
 {
     using S = typename Elem<SD>::t;
     using B = typename Elem<BD>::t;
-    __shared__ float2 lds[NW];
+    __shared__ float2 lds[NT / 64];
     const int64_t D = p.d.D;
     const bool layer = p.d.kind == RTP_NORM_LAYER, join = p.d.parts & RTP_NORM_JOIN, post = p.d.parts & RTP_NORM_POST, pre = p.d.parts & RTP_NORM_PRE;
     const float inv = 1.0f / (float)D;
@@ -126,7 +280,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_row_kernel(NormBwd p)
                 a += dn;
                 b += dn * ((float)r[i] - st.z) * st.w;
             }
-            m1 = group_sum(a, b, lds);
+            m1 = group_sum<NT / 64>(a, b, lds);
             m1 = {layer ? m1.x * inv : 0.0f, m1.y * inv};
         }
         // gradient of the stream's row at i
@@ -152,7 +306,7 @@ __global__ __launch_bounds__(NT) void norm_bwd_row_kernel(NormBwd p)
                 a += dn;
                 b += dn * ((float)y[i] - st.x) * st.y;
             }
-            m2 = group_sum(a, b, lds);
+            m2 = group_sum<NT / 64>(a, b, lds);
             m2 = {layer ? m2.x * inv : 0.0f, m2.y * inv};
         }
         for (int64_t i = threadIdx.x; i < D; i += NT) {
@@ -221,11 +375,38 @@ static hipError_t by_types(const rtp_norm_desc &d, F f)
     return f.template operator()<RTP_F16, RTP_F16>();
 }
 
+// Threads that share a row held in registers, and the eights a thread has of it.
+template <class F>
+static hipError_t by_length(int64_t D, F f)
+{
+    if (D <= 512) return f.template operator()<64, 1>();
+    if (D <= 1024) return f.template operator()<64, 2>();
+    if (D <= 2048) return f.template operator()<256, 1>();
+    if (D <= 4096) return f.template operator()<256, 2>();
+    if (D <= 8192) return f.template operator()<512, 2>();
+    return f.template operator()<1024, 2>();
+}
+constexpr int64_t NORM_REG_D = 16384;
+
+template <rtp_dtype SD, rtp_dtype BD> struct RunFwdRegs {
+    const NormFwd &p;
+    hipStream_t s;
+    template <int THREADS, int NV> hipError_t operator()()
+    {
+        constexpr int BLOCK = norm_block<THREADS>(), ROWS = BLOCK / THREADS;
+        const unsigned grid = (unsigned)std::min<int64_t>((p.d.T + ROWS - 1) / ROWS, std::max(256, 256 * 768 / BLOCK));
+        if (p.d.b_post_dev || p.d.b_pre_dev) norm_fwd_kernel<SD, BD, THREADS, NV, true><<<grid, BLOCK, 0, s>>>(p);
+        else norm_fwd_kernel<SD, BD, THREADS, NV, false><<<grid, BLOCK, 0, s>>>(p);
+        return hipGetLastError();
+    }
+};
+
 struct RunFwd {
     const NormFwd &p;
     hipStream_t s;
     template <rtp_dtype SD, rtp_dtype BD> hipError_t operator()()
     {
+        if (p.d.D <= NORM_REG_D) return by_length(p.d.D, RunFwdRegs<SD, BD>{p, s});
         norm_fwd_row_kernel<SD, BD><<<(unsigned)std::min<int64_t>(p.d.T, 1 << 20), NT, 0, s>>>(p);
         return hipGetLastError();
     }
