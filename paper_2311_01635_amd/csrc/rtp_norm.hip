@@ -249,6 +249,179 @@ struct NormBwd {
     int nsums;
 };
 
+// Rows in registers.  Bound: HBM.  The sums over rows stay in registers too, a thread's columns over all rows of its workgroup, so
+// that they cost one write a workgroup (and one read by norm_sums_kernel, which adds the workgroups up in a fixed order).
+// With k = out_scale gate w_post and q = dR k g (g: an element gate): dy = rs (q - mean q - n mean(q n)).
+template <rtp_dtype SD, rtp_dtype BD, int THREADS, int NV, bool BIAS>
+__global__ __launch_bounds__(norm_block<THREADS>()) void norm_bwd_kernel(NormBwd p)
+{
+    using S = typename Elem<SD>::t;
+    using B = typename Elem<BD>::t;
+    constexpr int WAVES = THREADS / 64, ROWS = norm_block<THREADS>() / THREADS;
+    __shared__ float2 lds[WAVES];
+    const int tid = threadIdx.x % THREADS;
+    const int64_t D = p.d.D;
+    const bool layer = p.d.kind == RTP_NORM_LAYER, join = p.d.parts & RTP_NORM_JOIN, post = p.d.parts & RTP_NORM_POST, pre = p.d.parts & RTP_NORM_PRE;
+    const bool elem = p.d.gate == RTP_GATE_ELEMENT, has_y = post || p.d.gate != RTP_GATE_NONE;
+    const float inv = 1.0f / (float)D, out_scale = join ? p.d.out_scale : 0.0f, res_scale = join ? p.d.res_scale : 1.0f;
+    int64_t at[NV], left[NV];
+    float w[NV][8], k2[NV][8];
+    float s1[NV][8], s2[NV][8], q1[NV][8], q2[NV][8]; // sums over rows: dh n, f n, dh, f, with f = out_scale dR (times an element gate)
+#pragma unroll
+    for (int j = 0; j < NV; ++j) {
+        at[j] = (tid + j * THREADS) * 8;
+        left[j] = D - at[j];
+        float g[8];
+        load_params(w[j], p.d.w_pre_dev, at[j], left[j], 1.0f);
+        load_params(k2[j], p.d.w_post_dev, at[j], left[j], 1.0f);
+        load_params(g, p.d.gate == RTP_GATE_CHANNEL ? (const float *)p.d.gate_dev : nullptr, at[j], left[j], 1.0f);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            k2[j][k] *= out_scale * g[k];
+            s1[j][k] = s2[j][k] = q1[j][k] = q2[j][k] = 0.0f;
+        }
+    }
+    for (int64_t row = (int64_t)blockIdx.x * ROWS + threadIdx.x / THREADS; row < p.d.T; row += (int64_t)gridDim.x * ROWS) {
+        Eight<SD> r[NV], dr[NV];
+        Eight<BD> y[NV], dh[NV], g[NV];
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (left[j] <= 0) continue;
+            if (pre) {
+                r[j].load((const S *)p.g.r_dev + row * p.g.ld_r + at[j], left[j]);
+                dh[j].load((const B *)p.g.dh_dev + row * p.g.ld_dh + at[j], left[j]);
+            }
+            if (p.g.dr_dev) dr[j].load((const S *)p.g.dr_dev + row * p.g.ld_dr + at[j], left[j]);
+            if (has_y) y[j].load((const B *)p.g.y_dev + row * p.g.ld_y + at[j], left[j]);
+            if (elem) g[j].load((const B *)p.d.gate_dev + row * p.d.ld_gate + at[j], left[j]);
+        }
+        float4 st = {0.0f, 1.0f, 0.0f, 1.0f};
+        if (post) { st.x = p.g.stats_dev[row * 4]; st.y = p.g.stats_dev[row * 4 + 1]; }
+        if (pre) { st.z = p.g.stats_dev[row * 4 + 2]; st.w = p.g.stats_dev[row * 4 + 3]; }
+        float v[NV][8]; // dR
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) v[j][k] = left[j] > 0 && p.g.dr_dev ? dr[j].get(k) : 0.0f;
+        if (pre) {
+            float a = 0.0f, b = 0.0f;
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (left[j] <= 0) continue;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) { // (behind the row's end dh is zero)
+                    const float d = dh[j].get(k), n = (r[j].get(k) - st.z) * st.w, dn = d * w[j][k];
+                    a += dn;
+                    b += dn * n;
+                    s1[j][k] += d * n;
+                    if (BIAS) q1[j][k] += d;
+                }
+            }
+            float2 m = group_sum<WAVES>(a, b, lds);
+            m = {layer ? m.x * inv : 0.0f, m.y * inv};
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (left[j] <= 0) continue;
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float n = (r[j].get(k) - st.z) * st.w;
+                    v[j][k] += st.w * (dh[j].get(k) * w[j][k] - m.x - n * m.y);
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (left[j] <= 0) continue;
+            float o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) o[k] = res_scale * v[j][k];
+            Eight<SD> dx;
+            dx.set(o);
+            dx.store((S *)p.g.dx_dev + row * p.g.ld_dx + at[j], left[j]);
+        }
+        if (!join) continue;
+        if (elem && p.g.dgate_dev) {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (left[j] <= 0) continue;
+                float o[8], c[8];
+                load_params(c, p.d.b_post_dev, at[j], left[j], 0.0f);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) o[k] = v[j][k] * ((y[j].get(k) - st.x) * st.y * k2[j][k] + out_scale * c[k]);
+                Eight<BD> dg;
+                dg.set(o);
+                dg.store((B *)p.g.dgate_dev + row * p.g.ld_dgate + at[j], left[j]);
+            }
+        }
+        float a = 0.0f, b = 0.0f;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (left[j] <= 0) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (elem) v[j][k] *= g[j].get(k); // (behind the row's end the gate is zero, but dR need not be)
+                else if (k >= left[j]) v[j][k] = 0.0f;
+                const float n = has_y ? (y[j].get(k) - st.x) * st.y : 0.0f, f = out_scale * v[j][k], q = v[j][k] * k2[j][k];
+                s2[j][k] += f * n;
+                if (BIAS) q2[j][k] += f;
+                a += q;
+                b += q * n;
+            }
+        }
+        float2 m = {0.0f, 0.0f};
+        if (post) {
+            m = group_sum<WAVES>(a, b, lds);
+            m = {layer ? m.x * inv : 0.0f, m.y * inv};
+        }
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            if (left[j] <= 0) continue;
+            float o[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float n = has_y ? (y[j].get(k) - st.x) * st.y : 0.0f;
+                o[k] = st.y * (v[j][k] * k2[j][k] - m.x - n * m.y);
+            }
+            Eight<BD> dy;
+            dy.set(o);
+            dy.store((B *)p.g.dy_dev + row * p.g.ld_dy + at[j], left[j]);
+        }
+    }
+    float *ws = (float *)p.g.ws_dev + (int64_t)blockIdx.x * p.nsums * D;
+    auto put = [&](const float (&v)[NV][8]) {
+        if (ROWS > 1) { // the workgroup's rows are apart by whole waves: joined in LDS
+            __shared__ float part[ROWS > 1 ? ROWS * THREADS * NV * 8 : 1];
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) part[((threadIdx.x / THREADS) * NV * 8 + j * 8 + k) * THREADS + tid] = v[j][k];
+            __syncthreads();
+            for (int i = threadIdx.x; i < NV * 8 * THREADS; i += ROWS * THREADS) {
+                const int t = i % THREADS, k = i / THREADS % 8, j = i / THREADS / 8; // thread t's column at 8 (t + j THREADS) + k
+                const int64_t col = (int64_t)(t + j * THREADS) * 8 + k;
+                float x = 0.0f;
+#pragma unroll
+                for (int q = 0; q < ROWS; ++q) x += part[(q * NV * 8 + j * 8 + k) * THREADS + t];
+                if (col < D) ws[col] = x;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < NV; ++j) {
+                if (left[j] <= 0) continue;
+                Eight<RTP_F32> e;
+                e.set(v[j]);
+                e.store(ws + at[j], left[j]);
+            }
+        }
+        ws += D;
+    };
+    if (p.sums & SUM_PRE_W) put(s1);
+    if (BIAS && p.sums & SUM_PRE_B) put(q1);
+    if (p.sums & SUM_POST_W) put(s2);
+    if (BIAS && p.sums & SUM_POST_B) put(q2);
+}
+
 // A workgroup takes every gridDim.x-th row and keeps its column sums in its own part of the workspace, where each column is
 // one thread's.
 template <rtp_dtype SD, rtp_dtype BD>
@@ -339,19 +512,37 @@ struct NormSums {
     int accumulate;
 };
 
-// The parts' column sums, in order, and the gradients that follow from them: with a channel gate the sums over rows leave it
-// out, S = sum of b dR n and Q = sum of b dR, so that dw = gate S, db = gate Q, dgate = w S + b Q.
-__global__ __launch_bounds__(NT) void norm_sums_kernel(NormSums p)
+// The parts' column sums, and the gradients that follow from them: with a channel gate the sums over rows leave it out, S = sum of
+// b dR n and Q = sum of b dR, so that dw = gate S, db = gate Q, dgate = w S + b Q.  Bound: latency (a few MB out of the caches).  16
+// columns a workgroup, 64 threads to each of them, so that a thread has few loads and all of them in flight; the
+// order of the additions is fixed.
+constexpr int SUM_COLS = 16, SUM_THREADS = 1024, SUM_GROUPS = SUM_THREADS / SUM_COLS;
+__global__ __launch_bounds__(SUM_THREADS) void norm_sums_kernel(NormSums p)
 {
-    const int64_t i = (int64_t)blockIdx.x * NT + threadIdx.x;
-    if (i >= p.D) return;
-    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    __shared__ float lds[4][SUM_THREADS / 64][SUM_COLS];
+    const int col = threadIdx.x % SUM_COLS, group = threadIdx.x / SUM_COLS;
+    const int64_t i = (int64_t)blockIdx.x * SUM_COLS + col;
     int at = 0;
+#pragma unroll
     for (int k = 0; k < 4; ++k) {
         if (!(p.sums >> k & 1)) continue;
-        for (int b = 0; b < p.parts; ++b) v[k] += p.ws[((int64_t)b * p.nsums + at) * p.D + i];
+        float v = 0.0f;
+        if (i < p.D) {
+#pragma unroll 4
+            for (int b = group; b < p.parts; b += SUM_GROUPS) v += p.ws[((int64_t)b * p.nsums + at) * p.D + i];
+        }
         ++at;
+        v += __shfl_xor(v, 16);
+        v += __shfl_xor(v, 32);
+        if (threadIdx.x % 64 < SUM_COLS) lds[k][threadIdx.x / 64][col] = v;
     }
+    __syncthreads();
+    if (threadIdx.x >= SUM_COLS || i >= p.D) return;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+        if (p.sums >> k & 1)
+            for (int w = 0; w < SUM_THREADS / 64; ++w) v[k] += lds[k][w][col];
     auto put = [&](float *to, float x) {
         if (to) to[i] = p.accumulate ? to[i] + x : x;
     };
@@ -377,7 +568,7 @@ static hipError_t by_types(const rtp_norm_desc &d, F f)
 
 // Threads that share a row held in registers, and the eights a thread has of it.
 template <class F>
-static hipError_t by_length(int64_t D, F f)
+static hipError_t by_length(int64_t D, F &&f)
 {
     if (D <= 512) return f.template operator()<64, 1>();
     if (D <= 1024) return f.template operator()<64, 2>();
@@ -418,13 +609,43 @@ hipError_t launch_norm_fwd(const rtp_norm_desc &d, const rtp_norm_io &io, hipStr
     return by_types(d, RunFwd{p, s});
 }
 
-int norm_bwd_parts(const rtp_norm_desc &d) { return (int)std::min<int64_t>(d.T, 1024); }
+// Workgroups of the backward pass: two to a compute unit (one of 512 threads and more), each of which leaves its sums.
+struct Parts {
+    int64_t T;
+    template <int THREADS, int NV> hipError_t operator()()
+    {
+        constexpr int BLOCK = norm_block<THREADS>(), ROWS = BLOCK / THREADS;
+        T = std::min<int64_t>((T + ROWS - 1) / ROWS, BLOCK > 256 ? 256 : 512);
+        return hipSuccess;
+    }
+};
+int norm_bwd_parts(const rtp_norm_desc &d)
+{
+    if (d.D > NORM_REG_D) return (int)std::min<int64_t>(d.T, 1024);
+    Parts parts{d.T};
+    (void)by_length(d.D, parts);
+    return (int)parts.T;
+}
+
+template <rtp_dtype SD, rtp_dtype BD> struct RunBwdRegs {
+    const NormBwd &p;
+    hipStream_t s;
+    template <int THREADS, int NV> hipError_t operator()()
+    {
+        constexpr int BLOCK = norm_block<THREADS>();
+        const unsigned grid = (unsigned)norm_bwd_parts(p.d);
+        if (p.sums & (SUM_PRE_B | SUM_POST_B)) norm_bwd_kernel<SD, BD, THREADS, NV, true><<<grid, BLOCK, 0, s>>>(p);
+        else norm_bwd_kernel<SD, BD, THREADS, NV, false><<<grid, BLOCK, 0, s>>>(p);
+        return hipGetLastError();
+    }
+};
 
 struct RunBwd {
     const NormBwd &p;
     hipStream_t s;
     template <rtp_dtype SD, rtp_dtype BD> hipError_t operator()()
     {
+        if (p.d.D <= NORM_REG_D) return by_length(p.d.D, RunBwdRegs<SD, BD>{p, s});
         norm_bwd_row_kernel<SD, BD><<<norm_bwd_parts(p.d), NT, 0, s>>>(p);
         return hipGetLastError();
     }
@@ -455,7 +676,7 @@ hipError_t launch_norm_bwd(const rtp_norm_desc &d, const rtp_norm_grads &g, unsi
     q.w_post = d.parts & RTP_NORM_POST ? d.w_post_dev : nullptr;
     q.b_post = d.parts & RTP_NORM_POST ? d.b_post_dev : nullptr;
     q.accumulate = g.accumulate;
-    norm_sums_kernel<<<(unsigned)((d.D + NT - 1) / NT), NT, 0, s>>>(q);
+    norm_sums_kernel<<<(unsigned)((d.D + SUM_COLS - 1) / SUM_COLS), SUM_THREADS, 0, s>>>(q);
     return hipGetLastError();
 }
 
