@@ -754,6 +754,7 @@ rtp_status rtp_norm_bwd(const rtp_norm_desc *d, const rtp_norm_grads *g, void *s
  * between rtp_ring_flush and rtp_ring_zero_grads), norms, a router's matrix.
  *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
+ * in fp32; under the root a second moment below 2^-126 counts as zero.
  * g: the fp32 gradient, times *scale_dev where that is given (clipping).
  * p: the fp32 master copy if there is one (the parameter is then its value,
  * rounded to nearest), else the parameter itself, 16-bit ones rounded at random
@@ -803,7 +804,7 @@ rtp_status rtp_adamw_create(rtp_adamw **out, const rtp_adamw_desc *desc);
 rtp_status rtp_adamw_destroy(rtp_adamw *opt);
 
 typedef struct {
-    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps > 0                         */
+    double lr, beta1, beta2, eps; /* 0 <= beta < 1, eps >= 2^-126                   */
     int64_t step;                 /* 1 for the first                                */
     uint32_t seed;
 } rtp_adamw_hyper;

@@ -5,136 +5,217 @@
 
 namespace rtp {
 
-constexpr int AT = RTP_ADAMW_BLOCK; // a thread an element of a block
+// Bound: HBM, 12 to 30 bytes a parameter that are read and written once.  With 8-bit moments the arithmetic is as long: at 6 TB/s a
+// parameter's 12 bytes leave a compute unit time for 79 instructions a wave, and the hash, the update and two
+// conversions are about 70 of them.  A wave takes four blocks of 256, a lane four neighbours of each: their 16 loads are sent
+// before the first is waited for, a block's largest element is a reduction within the wave, and nothing needs a barrier.
+constexpr int AT = 256, AB = 4; // threads, blocks of a wave
+static_assert(AT / 64 * AB == ADAMW_CHUNK_BLOCKS, "a workgroup is a chunk");
 
 // ---- moments in 8 bits -----------------------------------------------------------------------
 // A code, shifted to where an fp32 has exponent and mantissa, is that number times a power of two, denormal ones included: reading
 // is a shift and a scaling, writing a scaling, an addition of random bits below the last kept one, and a shift.
 constexpr int TOP_M = 14, TOP_V = 30; // exponent code of the binade of a block's largest element (one above is for a carry)
 
-__device__ __forceinline__ float unpack(unsigned mag, int E, int top)
+// byte k of a word of codes; `scale` = E - TOP
+__device__ __forceinline__ float unpack_m(uint32_t word, int k, int scale)
 {
-    return E == 255 ? __builtin_nanf("") : ldexpf(__uint_as_float(mag << 20), E - top);
+    return ldexpf(__uint_as_float((uint32_t)((int32_t)(word << (24 - 8 * k)) >> 4) & 0x87F00000u), scale);
 }
-__device__ __forceinline__ unsigned pack(float a, int E, int top, unsigned rnd16)
+__device__ __forceinline__ float unpack_v(uint32_t word, int k, int scale)
 {
-    return (__float_as_uint(ldexpf(a, top - E)) + (rnd16 << 4)) >> 20;
+    return ldexpf(__uint_as_float((word >> 8 * k & 255u) << 20), scale);
+}
+__device__ __forceinline__ uint32_t pack(float a, int scale, uint32_t rnd16)
+{
+    return (__float_as_uint(ldexpf(a, scale)) + (rnd16 << 4)) >> 20;
 }
 
-// 32 random bits of the seed and an element's place, and 16 more
-__device__ __forceinline__ unsigned hash(unsigned place, unsigned seed)
+// 32 random bits of the seed and an element's place (x = place * PLACE + seed), and 16 more
+constexpr uint32_t PLACE = 0x9E3779B1u;
+__device__ __forceinline__ uint32_t hash(uint32_t x)
 {
-    unsigned x = place * 0x9E3779B1u + seed;
     x = (x ^ x >> 15) * 0xB504F333u;
     x = (x ^ x >> 16) * 0x243F6A89u;
     return x ^ x >> 15;
 }
-__device__ __forceinline__ unsigned hash_more(unsigned x) { return x * 0x9E3779B1u >> 16; }
+__device__ __forceinline__ uint32_t hash_more(uint32_t x) { return x * 0x9E3779B1u >> 16; }
 
-// a float between two neighbours of a 16-bit type goes to the upper with the probability of its place between them
-__device__ __forceinline__ float round_random(float v, rtp_dtype t, unsigned rnd16)
+// A float between two neighbours of a 16-bit type goes to the upper with the probability of its place between them.  (Infinities have no
+// bits below to carry; NaN, which may, are let through.)
+template <rtp_dtype D> __device__ __forceinline__ float round_random(float v, uint32_t rnd16)
 {
-    const unsigned u = __float_as_uint(v);
-    if ((u & 0x7F800000u) == 0x7F800000u) return v;
-    if (t == RTP_BF16) return __uint_as_float((u + rnd16) & 0xFFFF0000u);
+    const uint32_t u = __float_as_uint(v);
+    if (D == RTP_BF16) return __uint_as_float((u + (v != v ? 0u : rnd16)) & 0xFFFF0000u);
+    if (!(fabsf(v) < INFINITY)) return v;
     if (fabsf(v) >= 6.103515625e-05f) return __uint_as_float((u + (rnd16 >> 3)) & 0xFFFFE000u);
     // below 2^-14 fp16's spacing is 2^-24
     const float n = floorf(ldexpf(fabsf(v), 24) + ldexpf((float)rnd16, -16));
     return copysignf(ldexpf(n, -24), v);
 }
 
-template <rtp_moments MO>
-__global__ __launch_bounds__(AT) void adamw_block_kernel(AdamwArgs p)
+// Blocks [first, first + AB) of a tensor's, as many as it has.
+template <rtp_moments MO, rtp_dtype D, bool MASTER>
+__device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntry &e, const int64_t first, const rtp_adamw_scalars &h, const float scale)
 {
-    __shared__ float high[2][AT / 64];
-    const rtp_adamw_scalars h = p.sc_dev ? *p.sc_dev : p.sc;
-    const float scale = p.scale ? *p.scale : 1.0f;
-    if (!(fabsf(scale) < INFINITY)) return;
-    for (int64_t chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
-        const AdamwEntry &e = p.entries[p.owner[chunk]];
-        const int64_t first = (chunk - e.chunk) * ADAMW_CHUNK;
-        for (int b = 0; b < ADAMW_CHUNK_BLOCKS && first + b * RTP_ADAMW_BLOCK < e.numel; ++b) {
-            const int64_t i = first + b * RTP_ADAMW_BLOCK + threadIdx.x, block = e.block + i / RTP_ADAMW_BLOCK;
-            const int64_t place = e.block * RTP_ADAMW_BLOCK + i;
-            const bool on = i < e.numel;
-            const float g = on ? e.grad[i] * scale : 0.0f;
-            float m, v;
-            if (MO == RTP_MOMENTS_F32) {
-                m = on ? ((const float *)p.m)[place] : 0.0f;
-                v = on ? ((const float *)p.v)[place] : 0.0f;
-            } else {
-                const unsigned mc = ((const uint8_t *)p.m)[place], vc = ((const uint8_t *)p.v)[place];
-                m = unpack(mc & 127, max((int)p.exps[block * 2], 1), TOP_M);
-                m = mc & 128 ? -m : m;
-                v = unpack(vc, max((int)p.exps[block * 2 + 1], 1), TOP_V);
-                if (!on) m = v = 0.0f;
-            }
-            m = h.beta1 * m + h.one_minus_beta1 * g;
-            v = h.beta2 * v + h.one_minus_beta2 * (g * g);
-            const unsigned rnd = hash((unsigned)place, h.seed);
-            if (on) {
-                float w = e.master ? e.master[i] : e.dtype == RTP_F32 ? ((const float *)e.param)[i] :
-                          e.dtype == RTP_BF16 ? (float)((const __bf16 *)e.param)[i] : (float)((const _Float16 *)e.param)[i];
-                w = w * (1.0f - h.lr * e.weight_decay) - h.step_size * (m / (sqrtf(v) * h.root_scale + h.eps));
-                if (e.master) e.master[i] = w;
-                else if (e.dtype != RTP_F32) w = round_random(w, (rtp_dtype)e.dtype, hash_more(rnd));
-                if (e.dtype == RTP_F32) ((float *)e.param)[i] = w;
-                else if (e.dtype == RTP_BF16) ((__bf16 *)e.param)[i] = (__bf16)w;
-                else ((_Float16 *)e.param)[i] = (_Float16)w;
-            }
-            if (MO == RTP_MOMENTS_F32) {
-                if (on) { ((float *)p.m)[place] = m; ((float *)p.v)[place] = v; }
-            } else {
-                // (magnitudes as integers are in the order of their values, NaN above all)
-                unsigned a = __float_as_uint(m) & 0x7FFFFFFFu, c = __float_as_uint(v) & 0x7FFFFFFFu;
+    using P = typename Elem<D>::t;
+    constexpr bool BYTE = MO == RTP_MOMENTS_8BIT, RANDOM = D != RTP_F32 && !MASTER;
+    const int lane = threadIdx.x & 63;
+    P *const param = (P *)e.param;
+    const float keep = 1.0f - h.lr * e.weight_decay;
+    Four<RTP_F32> g[AB], master[AB], fm[AB], fv[AB];
+    Four<D> w[AB];
+    uint32_t bm[AB], bv[AB], ex[AB];
+    int64_t at[AB], left[AB];
 #pragma unroll
-                for (int o = 32; o; o >>= 1) { a = max(a, (unsigned)__shfl_xor((int)a, o)); c = max(c, (unsigned)__shfl_xor((int)c, o)); }
-                __syncthreads();
-                if ((threadIdx.x & 63) == 0) { high[0][threadIdx.x >> 6] = __uint_as_float(a); high[1][threadIdx.x >> 6] = __uint_as_float(c); }
-                __syncthreads();
-                for (int k = 0; k < AT / 64; ++k) { a = max(a, __float_as_uint(high[0][k])); c = max(c, __float_as_uint(high[1][k])); }
-                const int Em = max((int)(a >> 23), 1), Ev = max((int)(c >> 23), 1);
-                ((uint8_t *)p.m)[place] = (uint8_t)(pack(fabsf(m), Em, TOP_M, rnd & 0xFFFF) | (__float_as_uint(m) >> 31 << 7));
-                ((uint8_t *)p.v)[place] = (uint8_t)max(pack(v, Ev, TOP_V, rnd >> 16), v > 0.0f ? 1u : 0u);
-                if (threadIdx.x == 0) { p.exps[block * 2] = (uint8_t)Em; p.exps[block * 2 + 1] = (uint8_t)Ev; }
+    for (int b = 0; b < AB; ++b) {
+        at[b] = (first + b) * RTP_ADAMW_BLOCK + lane * 4;
+        left[b] = e.numel - at[b];
+        if ((first + b) * RTP_ADAMW_BLOCK >= e.numel) continue;
+        const int64_t place = e.block * RTP_ADAMW_BLOCK + at[b];
+        g[b].load(e.grad + at[b], left[b]);
+        if (MASTER) master[b].load(e.master + at[b], left[b]);
+        else w[b].load(param + at[b], left[b]);
+        if (BYTE) {
+            bm[b] = *(const uint32_t *)((const uint8_t *)p.m + place);
+            bv[b] = *(const uint32_t *)((const uint8_t *)p.v + place);
+            ex[b] = *(const uint16_t *)(p.exps + (e.block + first + b) * 2);
+        } else {
+            fm[b].load((const float *)p.m + place, 4);
+            fv[b].load((const float *)p.v + place, 4);
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < AB; ++b) {
+        if ((first + b) * RTP_ADAMW_BLOCK >= e.numel) continue;
+        const int64_t place = e.block * RTP_ADAMW_BLOCK + at[b];
+        const int em = max((int)(ex[b] & 255), 1), ev = max((int)(ex[b] >> 8), 1); // (8-bit moments alone)
+        float m[4], v[4], o[4];
+        uint32_t rnd[4], top_m = 0, top_v = 0;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float gr = g[b].get(k) * scale;
+            if (BYTE) {
+                m[k] = unpack_m(bm[b], k, em - TOP_M);
+                v[k] = unpack_v(bv[b], k, ev - TOP_V);
+                if (em == 255) m[k] = __builtin_nanf("");
+                if (ev == 255) v[k] = __builtin_nanf("");
+                if (k >= left[b]) m[k] = v[k] = 0.0f; // behind the tensor
+            } else {
+                m[k] = fm[b].get(k);
+                v[k] = fv[b].get(k);
             }
+            m[k] = fmaf(h.one_minus_beta1, gr, h.beta1 * m[k]);
+            v[k] = fmaf(h.one_minus_beta2 * gr, gr, h.beta2 * v[k]);
+            if (BYTE || RANDOM) rnd[k] = hash((uint32_t)(place + k) * PLACE + h.seed);
+            // the hardware's root and reciprocal, 1 ulp each (a second moment below 2^-126 counts as zero here)
+            const float d = m[k] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[k]), h.root_scale, h.eps));
+            o[k] = fmaf(-h.step_size, d, keep * (MASTER ? master[b].get(k) : w[b].get(k)));
+            if (BYTE) {
+                // (magnitudes as integers are in the order of their values, NaN above all)
+                top_m = max(top_m, __float_as_uint(m[k]) & 0x7FFFFFFFu);
+                top_v = max(top_v, __float_as_uint(v[k]) & 0x7FFFFFFFu);
+            }
+        }
+        if (MASTER) {
+            master[b].set(o);
+            master[b].store(e.master + at[b], left[b]);
+        }
+        if (RANDOM) {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) o[k] = round_random<D>(o[k], hash_more(rnd[k]));
+        }
+        w[b].set(o);
+        w[b].store(param + at[b], left[b]);
+        if (BYTE) {
+            const int Em = max((int)(wave_umax(top_m) >> 23), 1), Ev = max((int)(wave_umax(top_v) >> 23), 1);
+            uint32_t cm = 0, cv = 0;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t sign = __float_as_uint(m[k]) >> 31 << 7;
+                cm |= (pack(fabsf(m[k]), TOP_M - Em, rnd[k] & 0xFFFF) & 127u | sign) << 8 * k;
+                // (a second moment that is there does not vanish)
+                cv |= (max(pack(v[k], TOP_V - Ev, rnd[k] >> 16), min(__float_as_uint(v[k]), 1u)) & 255u) << 8 * k;
+            }
+            *(uint32_t *)((uint8_t *)p.m + place) = cm;
+            *(uint32_t *)((uint8_t *)p.v + place) = cv;
+            if (lane == 0) *(uint16_t *)(p.exps + (e.block + first + b) * 2) = (uint16_t)(Em | Ev << 8);
+        } else {
+            fm[b].set(m);
+            fv[b].set(v);
+            fm[b].store((float *)p.m + place, left[b]);
+            fv[b].store((float *)p.v + place, left[b]);
         }
     }
 }
 
+template <rtp_moments MO>
+__global__ __launch_bounds__(AT) void adamw_kernel(AdamwArgs p)
+{
+    const rtp_adamw_scalars h = p.sc_dev ? *p.sc_dev : p.sc;
+    const float scale = p.scale ? *p.scale : 1.0f;
+    if (!(fabsf(scale) < INFINITY)) return;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64);
+    for (int64_t chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
+        const AdamwEntry &e = p.entries[p.owner[chunk]];
+        const int64_t first = (chunk - e.chunk) * ADAMW_CHUNK_BLOCKS + wave * AB;
+        if (e.dtype == RTP_F32) adamw_blocks<MO, RTP_F32, false>(p, e, first, h, scale);
+        else if (e.dtype == RTP_BF16 && e.master) adamw_blocks<MO, RTP_BF16, true>(p, e, first, h, scale);
+        else if (e.dtype == RTP_BF16) adamw_blocks<MO, RTP_BF16, false>(p, e, first, h, scale);
+        else if (e.master) adamw_blocks<MO, RTP_F16, true>(p, e, first, h, scale);
+        else adamw_blocks<MO, RTP_F16, false>(p, e, first, h, scale);
+    }
+}
+
+// Moments as numbers.  Bound: HBM.  A thread takes 16 neighbours, a block 16 threads.
 template <rtp_moments MO, rtp_dtype DT>
 __global__ __launch_bounds__(AT) void adamw_moments_kernel(const void *m, const void *v, const uint8_t *exps, int64_t blocks, void *m_out, void *v_out)
 {
     using O = typename Elem<DT>::t;
-    for (int64_t b = blockIdx.x; b < blocks; b += gridDim.x) {
-        const int64_t i = b * RTP_ADAMW_BLOCK + threadIdx.x;
-        float x, y;
-        if (MO == RTP_MOMENTS_F32) {
-            x = ((const float *)m)[i];
-            y = ((const float *)v)[i];
-        } else {
-            const unsigned mc = ((const uint8_t *)m)[i];
-            x = unpack(mc & 127, max((int)exps[b * 2], 1), TOP_M);
-            x = mc & 128 ? -x : x;
-            y = unpack(((const uint8_t *)v)[i], max((int)exps[b * 2 + 1], 1), TOP_V);
+    const int64_t b = (int64_t)blockIdx.x * (AT / 16) + threadIdx.x / 16, i = b * RTP_ADAMW_BLOCK + threadIdx.x % 16 * 16;
+    if (b >= blocks) return;
+    float x[16], y[16];
+    if (MO == RTP_MOMENTS_F32) {
+#pragma unroll
+        for (int k = 0; k < 16; ++k) { x[k] = ((const float *)m)[i + k]; y[k] = ((const float *)v)[i + k]; }
+    } else {
+        const uint4 cm = *(const uint4 *)((const uint8_t *)m + i), cv = *(const uint4 *)((const uint8_t *)v + i);
+        const uint32_t wm[4] = {cm.x, cm.y, cm.z, cm.w}, wv[4] = {cv.x, cv.y, cv.z, cv.w};
+        const uint32_t ex = *(const uint16_t *)(exps + b * 2);
+        const int em = max((int)(ex & 255), 1), ev = max((int)(ex >> 8), 1);
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+            x[k] = em == 255 ? __builtin_nanf("") : unpack_m(wm[k / 4], k % 4, em - TOP_M);
+            y[k] = ev == 255 ? __builtin_nanf("") : unpack_v(wv[k / 4], k % 4, ev - TOP_V);
         }
-        ((O *)m_out)[i] = (O)x;
-        ((O *)v_out)[i] = (O)y;
+    }
+#pragma unroll
+    for (int k = 0; k < 16; k += 8) {
+        Eight<DT> e;
+        float t[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t[q] = x[k + q];
+        e.set(t);
+        e.store((O *)m_out + i + k, 8);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) t[q] = y[k + q];
+        e.set(t);
+        e.store((O *)v_out + i + k, 8);
     }
 }
 
 hipError_t launch_adamw(rtp_moments moments, const AdamwArgs &a, hipStream_t s)
 {
     const unsigned grid = (unsigned)std::min<int64_t>(a.chunks, 1 << 20);
-    if (moments == RTP_MOMENTS_F32) adamw_block_kernel<RTP_MOMENTS_F32><<<grid, AT, 0, s>>>(a);
-    else adamw_block_kernel<RTP_MOMENTS_8BIT><<<grid, AT, 0, s>>>(a);
+    if (moments == RTP_MOMENTS_F32) adamw_kernel<RTP_MOMENTS_F32><<<grid, AT, 0, s>>>(a);
+    else adamw_kernel<RTP_MOMENTS_8BIT><<<grid, AT, 0, s>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_adamw_moments(rtp_moments moments, rtp_dtype out, const void *m, const void *v, const uint8_t *exps, int64_t blocks,
                                 void *m_out, void *v_out, hipStream_t s)
 {
-    const unsigned grid = (unsigned)std::min<int64_t>(blocks, 1 << 20);
+    const unsigned grid = (unsigned)((blocks + AT / 16 - 1) / (AT / 16));
     const bool f = out == RTP_F32;
     if (moments == RTP_MOMENTS_F32) {
         if (f) adamw_moments_kernel<RTP_MOMENTS_F32, RTP_F32><<<grid, AT, 0, s>>>(m, v, exps, blocks, m_out, v_out);

@@ -4,6 +4,7 @@
 #include "rtp_error.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -261,7 +262,7 @@ static bool adamw_sizes(const rtp_adamw_tensor *t, int count, int64_t *blocks, i
         if (t[i].numel < 1 || t[i].numel > ((int64_t)1 << 40)) return false;
         *blocks += (t[i].numel + RTP_ADAMW_BLOCK - 1) / RTP_ADAMW_BLOCK;
         *chunks += (t[i].numel + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
-        if (*blocks > (int64_t)1 << 40) return false;
+        if (*blocks > (int64_t)1 << 28) return false; // (a grid of a workgroup for 16 of them)
     }
     return true;
 }
@@ -378,9 +379,9 @@ extern "C" rtp_status rtp_adamw_scalars_of(const rtp_adamw_hyper *h, rtp_adamw_s
 {
     const char *who = "rtp_adamw_scalars_of";
     if (!h || !out) return fail(RTP_ERR_INVALID, "%s: null argument", who);
-    if (!(h->beta1 >= 0 && h->beta1 < 1 && h->beta2 >= 0 && h->beta2 < 1) || !((float)h->eps > 0) || !std::isfinite((float)h->eps) ||
+    if (!(h->beta1 >= 0 && h->beta1 < 1 && h->beta2 >= 0 && h->beta2 < 1) || !((float)h->eps >= FLT_MIN) || !std::isfinite((float)h->eps) ||
         !std::isfinite((float)h->lr) || h->step < 1)
-        return fail(RTP_ERR_INVALID, "%s: need 0 <= beta < 1, eps > 0, a finite lr, step >= 1", who);
+        return fail(RTP_ERR_INVALID, "%s: need 0 <= beta < 1, eps of at least 2^-126, a finite lr, step >= 1", who);
     *out = rtp_adamw_scalars{};
     out->beta1 = (float)h->beta1;
     out->one_minus_beta1 = (float)(1.0 - h->beta1);
