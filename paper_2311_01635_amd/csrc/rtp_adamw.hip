@@ -2,13 +2,15 @@
 #include "rtp_block_kernels.h"
 #include "rtp_elem.h"
 #include <algorithm>
+#include <type_traits>
 
 namespace rtp {
 
 // Bound: HBM, 12 to 30 bytes a parameter that are read and written once.  With 8-bit moments the arithmetic is as long: at 6 TB/s a
 // parameter's 12 bytes leave a compute unit time for 79 instructions a wave, and the hash, the update and two
 // conversions are about 70 of them.  A wave takes four blocks of 256, a lane four neighbours of each: their 16 loads are sent
-// before the first is waited for, a block's largest element is a reduction within the wave, and nothing needs a barrier.
+// before the first is waited for (past the caches: 762 -> 706 us for 135M with fp32 moments and masters), a block's largest element is a
+// reduction within the wave, and nothing needs a barrier.
 constexpr int AT = 256, AB = 4; // threads, blocks of a wave
 static_assert(AT / 64 * AB == ADAMW_CHUNK_BLOCKS, "a workgroup is a chunk");
 
@@ -54,60 +56,80 @@ template <rtp_dtype D> __device__ __forceinline__ float round_random(float v, ui
     return copysignf(ldexpf(n, -24), v);
 }
 
-// Blocks [first, first + AB) of a tensor's, as many as it has.
-template <rtp_moments MO, rtp_dtype D, bool MASTER>
+// (a pointer out of the table is one into device memory: without the word for it the accesses are the flat ones, which wait for LDS too)
+template <class T> __device__ __forceinline__ T *global(T *p)
+{
+    return (T *)(__attribute__((address_space(1))) T *)(uintptr_t)p;
+}
+
+// Blocks [first, first + AB) of a tensor's, as many as it has.  FULL: all of them, whole.
+template <rtp_moments MO, rtp_dtype D, bool MASTER, bool FULL>
 __device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntry &e, const int64_t first, const rtp_adamw_scalars &h, const float scale)
 {
     using P = typename Elem<D>::t;
     constexpr bool BYTE = MO == RTP_MOMENTS_8BIT, RANDOM = D != RTP_F32 && !MASTER;
-    const int lane = threadIdx.x & 63;
-    P *const param = (P *)e.param;
+    const int i = (threadIdx.x & 63) * 4; // this lane's place in a block
+    const int64_t from = first * RTP_ADAMW_BLOCK, place = e.block * RTP_ADAMW_BLOCK + from;
+    const int total = FULL ? AB * RTP_ADAMW_BLOCK : (int)min(e.numel - from, (int64_t)AB * RTP_ADAMW_BLOCK);
+    P *const param = global((P *)e.param) + from;
+    const float *const grad = global(e.grad) + from;
+    float *const copy = global(e.master) + from, *const pm = (float *)p.m + place, *const pv = (float *)p.v + place;
+    uint8_t *const qm = (uint8_t *)p.m + place, *const qv = (uint8_t *)p.v + place;
+    uint16_t *const exps = (uint16_t *)p.exps + e.block + first;
     const float keep = 1.0f - h.lr * e.weight_decay;
     Four<RTP_F32> g[AB], master[AB], fm[AB], fv[AB];
     Four<D> w[AB];
     uint32_t bm[AB], bv[AB], ex[AB];
-    int64_t at[AB], left[AB];
 #pragma unroll
     for (int b = 0; b < AB; ++b) {
-        at[b] = (first + b) * RTP_ADAMW_BLOCK + lane * 4;
-        left[b] = e.numel - at[b];
-        if ((first + b) * RTP_ADAMW_BLOCK >= e.numel) continue;
-        const int64_t place = e.block * RTP_ADAMW_BLOCK + at[b];
-        g[b].load(e.grad + at[b], left[b]);
-        if (MASTER) master[b].load(e.master + at[b], left[b]);
-        else w[b].load(param + at[b], left[b]);
+        const int at = b * RTP_ADAMW_BLOCK;
+        if (!FULL && at >= total) break;
+        const int n = FULL ? 4 : total - at - i;
+        g[b].template load<true>(grad + at + i, n);
+        if (MASTER) master[b].template load<true>(copy + at + i, n);
+        else w[b].template load<true>(param + at + i, n);
         if (BYTE) {
-            bm[b] = *(const uint32_t *)((const uint8_t *)p.m + place);
-            bv[b] = *(const uint32_t *)((const uint8_t *)p.v + place);
-            ex[b] = *(const uint16_t *)(p.exps + (e.block + first + b) * 2);
+            bm[b] = __builtin_nontemporal_load((const uint32_t *)(qm + at + i));
+            bv[b] = __builtin_nontemporal_load((const uint32_t *)(qv + at + i));
+            ex[b] = exps[b];
         } else {
-            fm[b].load((const float *)p.m + place, 4);
-            fv[b].load((const float *)p.v + place, 4);
+            fm[b].template load<true>(pm + at + i, 4);
+            fv[b].template load<true>(pv + at + i, 4);
         }
     }
 #pragma unroll
     for (int b = 0; b < AB; ++b) {
-        if ((first + b) * RTP_ADAMW_BLOCK >= e.numel) continue;
-        const int64_t place = e.block * RTP_ADAMW_BLOCK + at[b];
-        const int em = max((int)(ex[b] & 255), 1), ev = max((int)(ex[b] >> 8), 1); // (8-bit moments alone)
+        const int at = b * RTP_ADAMW_BLOCK;
+        if (!FULL && at >= total) break;
+        const int n = FULL ? 4 : total - at - i;
         float m[4], v[4], o[4];
+        if (BYTE) {
+            const int x = __builtin_amdgcn_readfirstlane(ex[b]), em = max(x & 255, 1), ev = max(x >> 8, 1);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                m[k] = unpack_m(bm[b], k, em - TOP_M);
+                v[k] = unpack_v(bv[b], k, ev - TOP_V);
+                if (!FULL && k >= n) m[k] = v[k] = 0.0f; // behind the tensor
+            }
+            if (em == 255 || ev == 255) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    if (em == 255) m[k] = __builtin_nanf("");
+                    if (ev == 255) v[k] = __builtin_nanf("");
+                }
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { m[k] = fm[b].get(k); v[k] = fv[b].get(k); }
+        }
         uint32_t rnd[4], top_m = 0, top_v = 0;
+        const uint32_t x = (uint32_t)(place + at + i) * PLACE + h.seed;
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float gr = g[b].get(k) * scale;
-            if (BYTE) {
-                m[k] = unpack_m(bm[b], k, em - TOP_M);
-                v[k] = unpack_v(bv[b], k, ev - TOP_V);
-                if (em == 255) m[k] = __builtin_nanf("");
-                if (ev == 255) v[k] = __builtin_nanf("");
-                if (k >= left[b]) m[k] = v[k] = 0.0f; // behind the tensor
-            } else {
-                m[k] = fm[b].get(k);
-                v[k] = fv[b].get(k);
-            }
             m[k] = fmaf(h.one_minus_beta1, gr, h.beta1 * m[k]);
             v[k] = fmaf(h.one_minus_beta2 * gr, gr, h.beta2 * v[k]);
-            if (BYTE || RANDOM) rnd[k] = hash((uint32_t)(place + k) * PLACE + h.seed);
+            if (BYTE || RANDOM) rnd[k] = hash(x + k * PLACE);
             // the hardware's root and reciprocal, 1 ulp each (a second moment below 2^-126 counts as zero here)
             const float d = m[k] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[k]), h.root_scale, h.eps));
             o[k] = fmaf(-h.step_size, d, keep * (MASTER ? master[b].get(k) : w[b].get(k)));
@@ -119,14 +141,14 @@ __device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntr
         }
         if (MASTER) {
             master[b].set(o);
-            master[b].store(e.master + at[b], left[b]);
+            master[b].store(copy + at + i, n);
         }
         if (RANDOM) {
 #pragma unroll
             for (int k = 0; k < 4; ++k) o[k] = round_random<D>(o[k], hash_more(rnd[k]));
         }
         w[b].set(o);
-        w[b].store(param + at[b], left[b]);
+        w[b].store(param + at + i, n);
         if (BYTE) {
             const int Em = max((int)(wave_umax(top_m) >> 23), 1), Ev = max((int)(wave_umax(top_v) >> 23), 1);
             uint32_t cm = 0, cv = 0;
@@ -137,14 +159,14 @@ __device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntr
                 // (a second moment that is there does not vanish)
                 cv |= (max(pack(v[k], TOP_V - Ev, rnd[k] >> 16), min(__float_as_uint(v[k]), 1u)) & 255u) << 8 * k;
             }
-            *(uint32_t *)((uint8_t *)p.m + place) = cm;
-            *(uint32_t *)((uint8_t *)p.v + place) = cv;
-            if (lane == 0) *(uint16_t *)(p.exps + (e.block + first + b) * 2) = (uint16_t)(Em | Ev << 8);
+            __builtin_nontemporal_store(cm, (uint32_t *)(qm + at + i));
+            __builtin_nontemporal_store(cv, (uint32_t *)(qv + at + i));
+            if (i == 0) exps[b] = (uint16_t)(Em | Ev << 8);
         } else {
             fm[b].set(m);
             fv[b].set(v);
-            fm[b].store((float *)p.m + place, left[b]);
-            fv[b].store((float *)p.v + place, left[b]);
+            fm[b].store(pm + at + i, n);
+            fv[b].store(pv + at + i, n);
         }
     }
 }
@@ -159,49 +181,52 @@ __global__ __launch_bounds__(AT) void adamw_kernel(AdamwArgs p)
     for (int64_t chunk = blockIdx.x; chunk < p.chunks; chunk += gridDim.x) {
         const AdamwEntry &e = p.entries[p.owner[chunk]];
         const int64_t first = (chunk - e.chunk) * ADAMW_CHUNK_BLOCKS + wave * AB;
-        if (e.dtype == RTP_F32) adamw_blocks<MO, RTP_F32, false>(p, e, first, h, scale);
-        else if (e.dtype == RTP_BF16 && e.master) adamw_blocks<MO, RTP_BF16, true>(p, e, first, h, scale);
-        else if (e.dtype == RTP_BF16) adamw_blocks<MO, RTP_BF16, false>(p, e, first, h, scale);
-        else if (e.master) adamw_blocks<MO, RTP_F16, true>(p, e, first, h, scale);
-        else adamw_blocks<MO, RTP_F16, false>(p, e, first, h, scale);
+        const bool full = (first + AB) * RTP_ADAMW_BLOCK <= e.numel;
+        if (first * RTP_ADAMW_BLOCK >= e.numel) continue;
+        auto blocks = [&](auto dtype, auto master) {
+            if (full) adamw_blocks<MO, decltype(dtype)::value, decltype(master)::value, true>(p, e, first, h, scale);
+            else adamw_blocks<MO, decltype(dtype)::value, decltype(master)::value, false>(p, e, first, h, scale);
+        };
+        using std::false_type;
+        using std::true_type;
+        if (e.dtype == RTP_F32) blocks(std::integral_constant<rtp_dtype, RTP_F32>{}, false_type{});
+        else if (e.dtype == RTP_BF16 && e.master) blocks(std::integral_constant<rtp_dtype, RTP_BF16>{}, true_type{});
+        else if (e.dtype == RTP_BF16) blocks(std::integral_constant<rtp_dtype, RTP_BF16>{}, false_type{});
+        else if (e.master) blocks(std::integral_constant<rtp_dtype, RTP_F16>{}, true_type{});
+        else blocks(std::integral_constant<rtp_dtype, RTP_F16>{}, false_type{});
     }
 }
 
-// Moments as numbers.  Bound: HBM.  A thread takes 16 neighbours, a block 16 threads.
+// Moments as numbers.  Bound: HBM.  A thread takes eight neighbours, a block 32 threads (16 to a thread left holes of 16 bytes in what a
+// store instruction writes: 285 us instead of 160 for 135M of 8 bits).
 template <rtp_moments MO, rtp_dtype DT>
 __global__ __launch_bounds__(AT) void adamw_moments_kernel(const void *m, const void *v, const uint8_t *exps, int64_t blocks, void *m_out, void *v_out)
 {
     using O = typename Elem<DT>::t;
-    const int64_t b = (int64_t)blockIdx.x * (AT / 16) + threadIdx.x / 16, i = b * RTP_ADAMW_BLOCK + threadIdx.x % 16 * 16;
+    const int64_t b = (int64_t)blockIdx.x * (AT / 32) + threadIdx.x / 32, i = b * RTP_ADAMW_BLOCK + threadIdx.x % 32 * 8;
     if (b >= blocks) return;
-    float x[16], y[16];
+    float x[8], y[8];
     if (MO == RTP_MOMENTS_F32) {
+        Eight<RTP_F32> em, ev;
+        em.load<true>((const float *)m + i, 8);
+        ev.load<true>((const float *)v + i, 8);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) { x[k] = ((const float *)m)[i + k]; y[k] = ((const float *)v)[i + k]; }
+        for (int k = 0; k < 8; ++k) { x[k] = em.get(k); y[k] = ev.get(k); }
     } else {
-        const uint4 cm = *(const uint4 *)((const uint8_t *)m + i), cv = *(const uint4 *)((const uint8_t *)v + i);
-        const uint32_t wm[4] = {cm.x, cm.y, cm.z, cm.w}, wv[4] = {cv.x, cv.y, cv.z, cv.w};
-        const uint32_t ex = *(const uint16_t *)(exps + b * 2);
+        const uint2 cm = *(const uint2 *)((const uint8_t *)m + i), cv = *(const uint2 *)((const uint8_t *)v + i);
+        const uint32_t ex = ((const uint16_t *)exps)[b];
         const int em = max((int)(ex & 255), 1), ev = max((int)(ex >> 8), 1);
 #pragma unroll
-        for (int k = 0; k < 16; ++k) {
-            x[k] = em == 255 ? __builtin_nanf("") : unpack_m(wm[k / 4], k % 4, em - TOP_M);
-            y[k] = ev == 255 ? __builtin_nanf("") : unpack_v(wv[k / 4], k % 4, ev - TOP_V);
+        for (int k = 0; k < 8; ++k) {
+            x[k] = em == 255 ? __builtin_nanf("") : unpack_m(k < 4 ? cm.x : cm.y, k % 4, em - TOP_M);
+            y[k] = ev == 255 ? __builtin_nanf("") : unpack_v(k < 4 ? cv.x : cv.y, k % 4, ev - TOP_V);
         }
     }
-#pragma unroll
-    for (int k = 0; k < 16; k += 8) {
-        Eight<DT> e;
-        float t[8];
-#pragma unroll
-        for (int q = 0; q < 8; ++q) t[q] = x[k + q];
-        e.set(t);
-        e.store((O *)m_out + i + k, 8);
-#pragma unroll
-        for (int q = 0; q < 8; ++q) t[q] = y[k + q];
-        e.set(t);
-        e.store((O *)v_out + i + k, 8);
-    }
+    Eight<DT> e;
+    e.set(x);
+    e.store((O *)m_out + i, 8);
+    e.set(y);
+    e.store((O *)v_out + i, 8);
 }
 
 hipError_t launch_adamw(rtp_moments moments, const AdamwArgs &a, hipStream_t s)
@@ -215,7 +240,7 @@ hipError_t launch_adamw(rtp_moments moments, const AdamwArgs &a, hipStream_t s)
 hipError_t launch_adamw_moments(rtp_moments moments, rtp_dtype out, const void *m, const void *v, const uint8_t *exps, int64_t blocks,
                                 void *m_out, void *v_out, hipStream_t s)
 {
-    const unsigned grid = (unsigned)((blocks + AT / 16 - 1) / (AT / 16));
+    const unsigned grid = (unsigned)((blocks + AT / 32 - 1) / (AT / 32));
     const bool f = out == RTP_F32;
     if (moments == RTP_MOMENTS_F32) {
         if (f) adamw_moments_kernel<RTP_MOMENTS_F32, RTP_F32><<<grid, AT, 0, s>>>(m, v, exps, blocks, m_out, v_out);

@@ -262,7 +262,7 @@ static bool adamw_sizes(const rtp_adamw_tensor *t, int count, int64_t *blocks, i
         if (t[i].numel < 1 || t[i].numel > ((int64_t)1 << 40)) return false;
         *blocks += (t[i].numel + RTP_ADAMW_BLOCK - 1) / RTP_ADAMW_BLOCK;
         *chunks += (t[i].numel + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
-        if (*blocks > (int64_t)1 << 28) return false; // (a grid of a workgroup for 16 of them)
+        if (*blocks > (int64_t)1 << 26) return false; // (a grid of a workgroup for eight of them: 2^32 threads at 2^27)
     }
     return true;
 }
