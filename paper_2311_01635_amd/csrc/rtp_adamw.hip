@@ -140,6 +140,9 @@ __device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntr
             }
         }
         if (MASTER) {
+            // (fp16: the compiler would round the update to it by itself, and not what the master holds)
+#pragma unroll
+            for (int k = 0; k < 4; ++k) asm("" : "+v"(o[k]));
             master[b].set(o);
             master[b].store(copy + at + i, n);
         }
