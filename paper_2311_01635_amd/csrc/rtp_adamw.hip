@@ -89,8 +89,8 @@ __device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntr
         if (MASTER) master[b].template load<true>(copy + at + i, n);
         else w[b].template load<true>(param + at + i, n);
         if (BYTE) {
-            bm[b] = __builtin_nontemporal_load((const uint32_t *)(qm + at + i));
-            bv[b] = __builtin_nontemporal_load((const uint32_t *)(qv + at + i));
+            bm[b] = *(const uint32_t *)(qm + at + i);
+            bv[b] = *(const uint32_t *)(qv + at + i);
             ex[b] = exps[b];
         } else {
             fm[b].template load<true>(pm + at + i, 4);
@@ -162,8 +162,8 @@ __device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntr
                 // (a second moment that is there does not vanish)
                 cv |= (max(pack(v[k], TOP_V - Ev, rnd[k] >> 16), min(__float_as_uint(v[k]), 1u)) & 255u) << 8 * k;
             }
-            __builtin_nontemporal_store(cm, (uint32_t *)(qm + at + i));
-            __builtin_nontemporal_store(cv, (uint32_t *)(qv + at + i));
+            *(uint32_t *)(qm + at + i) = cm;
+            *(uint32_t *)(qv + at + i) = cv;
             if (i == 0) exps[b] = (uint16_t)(Em | Ev << 8);
         } else {
             fm[b].set(m);
