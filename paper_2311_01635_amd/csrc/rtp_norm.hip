@@ -277,12 +277,12 @@ __global__ __launch_bounds__(norm_block<THREADS>()) void norm_bwd_kernel(NormBwd
         for (int j = 0; j < NV; ++j) {
             if (left[j] <= 0) continue;
             if (pre) {
-                next_r[j].load((const S *)p.g.r_dev + i * p.g.ld_r + at[j], left[j]);
-                next_dh[j].load((const B *)p.g.dh_dev + i * p.g.ld_dh + at[j], left[j]);
+                next_r[j].template load<true>((const S *)p.g.r_dev + i * p.g.ld_r + at[j], left[j]);
+                next_dh[j].template load<true>((const B *)p.g.dh_dev + i * p.g.ld_dh + at[j], left[j]);
             }
-            if (p.g.dr_dev) next_dr[j].load((const S *)p.g.dr_dev + i * p.g.ld_dr + at[j], left[j]);
-            if (has_y) next_y[j].load((const B *)p.g.y_dev + i * p.g.ld_y + at[j], left[j]);
-            if (elem) next_g[j].load((const B *)p.d.gate_dev + i * p.d.ld_gate + at[j], left[j]);
+            if (p.g.dr_dev) next_dr[j].template load<true>((const S *)p.g.dr_dev + i * p.g.ld_dr + at[j], left[j]);
+            if (has_y) next_y[j].template load<true>((const B *)p.g.y_dev + i * p.g.ld_y + at[j], left[j]);
+            if (elem) next_g[j].template load<true>((const B *)p.d.gate_dev + i * p.d.ld_gate + at[j], left[j]);
         }
         if (post) { next_st.x = p.g.stats_dev[i * 4]; next_st.y = p.g.stats_dev[i * 4 + 1]; }
         if (pre) { next_st.z = p.g.stats_dev[i * 4 + 2]; next_st.w = p.g.stats_dev[i * 4 + 3]; }

@@ -6,7 +6,12 @@
 
 namespace rtp {
 
-constexpr int RW = 4; // waves of a workgroup, a row each
+// Bound: the arithmetic of the choice (a row of 256 is 1 KB; its eight largest are eight rounds of comparisons).  LANES lanes share
+// a row, eight or sixteen neighbouring experts each, 64 / LANES rows to a wave: a round is then a maximum over a lane's keys, one over
+// LANES lanes, and the lowest lane that has it, with no barrier and little LDS.  Keys are 32-bit integers in the order of what they
+// stand for.  Where the choice is of scores (a bias, groups), they are scores in 32 bits; a row in which two of them that
+// matter are closer than 32 bits can tell apart is decided again in 64 bits by its whole wave.
+constexpr int RW = 4; // waves of a workgroup
 
 struct RouteArgs {
     rtp_route_desc d;
@@ -19,16 +24,60 @@ struct RouteArgs {
     void *dlogits;
 };
 
-// What an expert is ranked by, as finite numbers: out of the choice (taken, of another group, not there) < closed < any choice < a NaN
-// logit.  (Beside a NaN logit every softmax is NaN: such choices are alike.)
-constexpr double KEY_NONE = -4e300, KEY_CLOSED = -1e300, KEY_NAN = 1e300;
+// log of a sigmoid, without the underflow of the sigmoid itself
+__device__ __forceinline__ float log_sigmoid(float l) { return fminf(l, 0.0f) - log1pf(expf(-fabsf(l))); }
 
-__device__ __forceinline__ double rank_key(double logit, double choice)
+// LDS operations of a wave are in order; this keeps the compiler from moving them past one another
+__device__ __forceinline__ void wave_fence() { __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront"); }
+
+// ---- over LANES neighbouring lanes, in each of them ----------------------------------------------
+template <int CTRL> __device__ __forceinline__ uint32_t dpp(uint32_t v)
 {
-    if (logit != logit) return KEY_NAN;
-    if (choice != choice) return 0.0;
-    return fmin(fmax(choice, KEY_CLOSED), 0.5 * KEY_NAN);
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
 }
+// f(own, other half's) for halves of 16 and of 32 lanes: the two results of a swap of a value with itself are both halves
+template <int HALF, class F> __device__ __forceinline__ uint32_t with_other_half(uint32_t v, F f)
+{
+    const auto r = HALF == 16 ? __builtin_amdgcn_permlane16_swap(v, v, false, false) : __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return f((uint32_t)r[0], (uint32_t)r[1]);
+}
+template <int LANES, class F> __device__ __forceinline__ uint32_t over(uint32_t v, F f)
+{
+    if (LANES >= 2) v = f(v, dpp<DPP_XOR1>(v));
+    if (LANES >= 4) v = f(v, dpp<DPP_XOR2>(v));
+    if (LANES >= 8) v = f(v, dpp<DPP_HALF_MIRROR>(v));
+    if (LANES >= 16) v = f(v, dpp<DPP_MIRROR>(v));
+    if (LANES >= 32) v = with_other_half<16>(v, f);
+    if (LANES >= 64) v = with_other_half<32>(v, f);
+    return v;
+}
+template <int LANES> __device__ __forceinline__ uint32_t over_max(uint32_t v)
+{
+    return over<LANES>(v, [](uint32_t a, uint32_t b) { return max(a, b); });
+}
+template <int LANES> __device__ __forceinline__ float over_fmax(float v)
+{
+    return __uint_as_float(over<LANES>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b))); }));
+}
+template <int LANES> __device__ __forceinline__ float over_sum(float v)
+{
+    return __uint_as_float(over<LANES>(__float_as_uint(v), [](uint32_t a, uint32_t b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }));
+}
+
+// ---- keys: 0 is out of the choice (taken, of another group, not there), 1 closed, then numbers in their order, NaN last ------
+constexpr uint32_t KEY_OUT = 0, KEY_CLOSED = 1, KEY_NAN = 0xFFFFFFFFu;
+__device__ __forceinline__ uint32_t key_of(float v)
+{
+    if (v != v) return KEY_NAN;
+    if (v == -INFINITY) return KEY_CLOSED;
+    const uint32_t u = __float_as_uint(v == 0.0f ? 0.0f : v); // (-0 and 0 are equal)
+    return u ^ ((int32_t)u < 0 ? 0xFFFFFFFFu : 0x80000000u);
+}
+__device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key ^ 0x80000000u : ~key); }
+
+// ---- one row in 64 bits, by a whole wave ------------------------------------------------------------
+// The same order as finite doubles.  Beside a NaN logit every softmax is NaN: such choices are alike.
+constexpr double ROW_OUT = -4e300, ROW_CLOSED = -1e300, ROW_NAN = 1e300;
 
 __device__ __forceinline__ double wave_max(double v)
 {
@@ -43,109 +92,244 @@ __device__ __forceinline__ double wave_add(double v)
     return v;
 }
 
-// log of a sigmoid, without the underflow of the sigmoid itself
-__device__ __forceinline__ float log_sigmoid(float l) { return fminf(l, 0.0f) - log1pf(expf(-fabsf(l))); }
-
-template <rtp_dtype DT>
-__global__ __launch_bounds__(64 * RW) void route_fwd_wave_kernel(RouteArgs p)
+template <class L>
+__device__ __forceinline__ void choose_in_64_bits(const rtp_route_desc &d, const L *l, const float *bias, double *key, double *group, int *slot_id, float *slot_l)
 {
-    using L = typename Elem<DT>::t;
-    __shared__ double keys[RW][RTP_ROUTE_MAX_EXPERTS];
-    __shared__ double group[RW][RTP_ROUTE_MAX_GROUPS];
-    __shared__ float slot_l[RW][RTP_ROUTE_MAX_TOP], slot_s[RW][RTP_ROUTE_MAX_TOP];
-    __shared__ int slot_id[RW][RTP_ROUTE_MAX_TOP];
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, E = p.d.E, k = p.d.k, G = p.d.groups, len = E / G;
-    const bool softmax = p.d.score == RTP_SCORE_SOFTMAX, scored = p.bias || G > 1;
-    double *key = keys[w];
-    for (int64_t row0 = (int64_t)blockIdx.x * RW; row0 < p.d.T; row0 += (int64_t)gridDim.x * RW) {
-        const int64_t row = row0 + w;
-        const bool on = row < p.d.T;
-        const L *l = (const L *)p.logits + (on ? row : 0) * p.d.ld;
-        double top = -INFINITY, sum = 0.0;
-        if (softmax) {
-            bool nan = false;
-            for (int e = lane; e < E; e += 64) {
-                const double v = (double)(float)l[e];
-                nan |= v != v;
-                top = fmax(top, v);
-            }
-            top = wave_max(top);
-            if (__any(nan)) top = NAN;
-            if (top == -INFINITY) top = 0.0;
-            for (int e = lane; e < E; e += 64) sum += exp((double)(float)l[e] - top);
-            sum = wave_add(sum);
-        }
-        auto score = [&](double v) {
-            return softmax ? (v == -INFINITY ? 0.0 : exp(v - top) / sum) : 1.0 / (1.0 + exp(-v));
-        };
+    const int lane = threadIdx.x & 63, E = d.E, G = d.groups, len = E / G;
+    const bool softmax = d.score == RTP_SCORE_SOFTMAX;
+    double top = -INFINITY, sum = 0.0;
+    if (softmax) {
+        bool nan = false;
         for (int e = lane; e < E; e += 64) {
             const double v = (double)(float)l[e];
-            key[e] = rank_key(v, !scored || v == -INFINITY ? v : score(v) + (p.bias ? (double)p.bias[e] : 0.0));
+            nan |= v != v;
+            top = fmax(top, v);
         }
-        __syncthreads();
-        if (G > 1) {
-            if (lane < G) { // a group's score
-                double a = KEY_NONE, b = KEY_NONE;
-                for (int i = 0; i < len; ++i) {
-                    const double v = key[lane * len + i];
-                    b = fmax(b, fmin(a, v));
-                    a = fmax(a, v);
-                }
-                group[w][lane] = p.d.group_top == 2 && b > KEY_CLOSED ? a + b : a;
+        top = wave_max(top);
+        if (__any(nan)) top = NAN;
+        if (top == -INFINITY) top = 0.0;
+        for (int e = lane; e < E; e += 64) sum += exp((double)(float)l[e] - top);
+        sum = wave_add(sum);
+    }
+    wave_fence();
+    for (int e = lane; e < E; e += 64) {
+        const double v = (double)(float)l[e];
+        const double c = v == -INFINITY ? v : (softmax ? exp(v - top) / sum : 1.0 / (1.0 + exp(-v))) + (bias ? (double)bias[e] : 0.0);
+        key[e] = v != v ? ROW_NAN : c != c ? 0.0 : fmin(fmax(c, ROW_CLOSED), 0.5 * ROW_NAN);
+    }
+    wave_fence();
+    if (G > 1) {
+        if (lane < G) { // a group's score
+            double a = ROW_OUT, b = ROW_OUT;
+            for (int i = 0; i < len; ++i) {
+                const double v = key[lane * len + i];
+                b = fmax(b, fmin(a, v));
+                a = fmax(a, v);
             }
-            __syncthreads();
-            for (int g = 0; g < G; ++g) {
-                int before = 0;
-                for (int o = 0; o < G; ++o) before += group[w][o] > group[w][g] || (group[w][o] == group[w][g] && o < g);
-                if (before >= p.d.kept_groups)
-                    for (int i = lane; i < len; i += 64) key[g * len + i] = KEY_NONE;
-            }
-            __syncthreads();
+            group[lane] = d.group_top == 2 && b > ROW_CLOSED ? a + b : a;
         }
-        for (int j = 0; j < k; ++j) {
-            double best = KEY_NONE;
-            int at = E;
-            for (int e = lane; e < E; e += 64)
-                if (key[e] > best) { best = key[e]; at = e; }
+        wave_fence();
+        for (int g = 0; g < G; ++g) {
+            int before = 0;
+            for (int o = 0; o < G; ++o) before += group[o] > group[g] || (group[o] == group[g] && o < g);
+            if (before >= d.kept_groups)
+                for (int i = lane; i < len; i += 64) key[g * len + i] = ROW_OUT;
+        }
+        wave_fence();
+    }
+    for (int j = 0; j < d.k; ++j) {
+        double best = ROW_OUT;
+        int at = E;
+        for (int e = lane; e < E; e += 64)
+            if (key[e] > best) { best = key[e]; at = e; }
 #pragma unroll
-            for (int o = 32; o; o >>= 1) {
-                const double b = __shfl_xor(best, o);
-                const int a = __shfl_xor(at, o);
-                if (b > best || (b == best && a < at)) { best = b; at = a; }
-            }
-            if (lane == 0) {
-                const float v = (float)l[at];
-                slot_id[w][j] = at;
-                slot_l[w][j] = v;
-                slot_s[w][j] = p.d.renormalise ? 0.0f : (float)score((double)v);
-                key[at] = KEY_NONE;
-            }
-            __syncthreads();
+        for (int o = 32; o; o >>= 1) {
+            const double b = __shfl_xor(best, o);
+            const int a = __shfl_xor(at, o);
+            if (b > best || (b == best && a < at)) { best = b; at = a; }
         }
-        if (on && lane < k) {
-            const float v = slot_l[w][lane];
-            float s;
+        wave_fence();
+        if (lane == 0) {
+            slot_id[j] = at;
+            slot_l[j] = (float)l[at];
+            key[at] = ROW_OUT;
+        }
+        wave_fence();
+    }
+}
+
+// SCORED: the choice is of scores.  EPL: experts of a lane.
+template <rtp_dtype DT, int LANES, int EPL, bool SCORED>
+__global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
+{
+    using L = typename Elem<DT>::t;
+    constexpr int ROWS = 64 / LANES, SLOTS = ROWS * (LANES * EPL < RTP_ROUTE_MAX_TOP ? LANES * EPL : RTP_ROUTE_MAX_TOP);
+    // a wave's keys in 64 bits and group scores, or its rows' in 32 bits
+    __shared__ double big[SCORED ? RW : 1][SCORED ? RTP_ROUTE_MAX_EXPERTS + RTP_ROUTE_MAX_GROUPS : 1];
+    __shared__ int slot_id[RW][SLOTS];
+    __shared__ float slot_l[RW][SLOTS];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, seg = lane / LANES, l = lane % LANES;
+    const int E = p.d.E, k = p.d.k, G = p.d.groups, len = E / G;
+    const bool softmax = p.d.score == RTP_SCORE_SOFTMAX;
+    int *const ids = slot_id[wave] + seg * k;
+    float *const ls = slot_l[wave] + seg * k;
+    const int left = E - l * EPL; // of this lane's experts that there are
+    for (int64_t row0 = ((int64_t)blockIdx.x * RW + wave) * ROWS; row0 < p.d.T; row0 += (int64_t)gridDim.x * RW * ROWS) {
+        const int64_t row = min(row0 + seg, p.d.T - 1);
+        const L *const logits = (const L *)p.logits + row * p.d.ld;
+        float v[EPL];
+#pragma unroll
+        for (int i = 0; i < EPL; i += 8) {
+            Eight<DT> x;
+            if (left > i) x.load(logits + l * EPL + i, left - i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i + e] = i + e < left ? x.get(e) : -INFINITY;
+        }
+        // sum over the row, which the scores of a softmax divide by
+        float top = -INFINITY, sum = 1.0f;
+        if (softmax && (SCORED || !p.d.renormalise)) {
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) top = fmaxf(top, v[e]);
+            top = over_fmax<LANES>(top);
+            if (top == -INFINITY) top = 0.0f;
+            sum = 0.0f;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) sum += expf(v[e] - top);
+            sum = over_sum<LANES>(sum);
+        }
+        uint32_t key[EPL];
+        bool unsure = false;
+        if (SCORED) {
+            const float inv = 1.0f / sum;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) {
+                const float b = p.bias && e < left ? p.bias[l * EPL + e] : 0.0f;
+                const float c = (softmax ? expf(v[e] - top) * inv : 1.0f / (1.0f + expf(-v[e]))) + b;
+                unsure |= e < left && (!(fabsf(c) < INFINITY) || v[e] == INFINITY) && v[e] != -INFINITY;
+                key[e] = v[e] == -INFINITY ? KEY_CLOSED : key_of(c);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) key[e] = key_of(v[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < EPL; ++e)
+            if (e >= left) key[e] = KEY_OUT;
+        // Two numbers closer than this may be in the other order.  A score is off by 2^-19 of itself at most (the 22 roundings of a
+        // sum of 1024 terms, the exponential and the quotient 3 more, and by a denormal), a choice by half a step of the row's largest
+        // on top: four times that.
+        float close = 0x1p-126f;
+        if (SCORED && p.bias) {
+            float most = 0.0f;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e)
+                if (key[e] > KEY_CLOSED) most = fmaxf(most, fabsf(value_of(key[e])));
+            close = 0x1p-17f * (softmax ? 1.0f / sum : 1.0f) + 0x1p-22f * over_fmax<LANES>(most);
+        }
+        auto apart = [&](float a) { return p.bias ? close : 0x1p-17f * a + close; };
+        if (SCORED && G > 1) {
+            uint32_t *const keys = (uint32_t *)big[wave] + seg * E;
+            float *const group = (float *)(big[wave] + RTP_ROUTE_MAX_EXPERTS / 2) + seg * G;
+            wave_fence();
+#pragma unroll
+            for (int e = 0; e < EPL; ++e)
+                if (e < left) keys[l * EPL + e] = key[e];
+            wave_fence();
+            // S lanes to a group
+            int S = LANES;
+            while (S > 1 && S * G > LANES) S >>= 1;
+            for (int g0 = 0; g0 < G; g0 += LANES / S) {
+                const int g = g0 + l / S;
+                uint32_t a = KEY_OUT, b = KEY_OUT;
+                if (g < G)
+                    for (int i = l % S; i < len; i += S) {
+                        const uint32_t x = keys[g * len + i];
+                        b = max(b, min(a, x));
+                        a = max(a, x);
+                    }
+                for (int o = 1; o < S; o <<= 1) {
+                    const uint32_t c = __shfl_xor(a, o), d = __shfl_xor(b, o);
+                    b = max(max(b, d), min(a, c));
+                    a = max(a, c);
+                }
+                if (g < G && l % S == 0)
+                    group[g] = a <= KEY_CLOSED ? -INFINITY : value_of(a) + (p.d.group_top == 2 && b > KEY_CLOSED ? value_of(b) : 0.0f);
+            }
+            wave_fence();
+            for (int g0 = 0; g0 < G; g0 += LANES / S) {
+                const int g = g0 + l / S;
+                if (g >= G) continue;
+                const float mine = group[g];
+                int before = 0;
+                for (int o = 0; o < G; ++o) {
+                    const float other = group[o];
+                    before += other > mine || (other == mine && o < g);
+                    unsure |= o != g && mine > -INFINITY && fabsf(other - mine) < 2.0f * apart(mine);
+                }
+                if (before >= p.d.kept_groups)
+                    for (int i = l % S; i < len; i += S) keys[g * len + i] = KEY_OUT;
+            }
+            wave_fence();
+#pragma unroll
+            for (int e = 0; e < EPL; ++e)
+                if (e < left) key[e] = keys[l * EPL + e];
+        }
+        uint32_t last = 0;
+        for (int j = 0; j < k + (SCORED ? 1 : 0); ++j) {
+            uint32_t best = KEY_OUT;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) best = max(best, key[e]);
+            const uint32_t most = over_max<LANES>(best);
+            if (SCORED) {
+                if (j > 0 && most > KEY_CLOSED) unsure |= value_of(last) - value_of(most) < apart(value_of(last));
+                last = most;
+                if (j == k) break;
+            }
+            // the lowest lane that has it, and its first key of that value
+            const uint64_t have = __ballot(best == most);
+            const uint64_t mine = LANES == 64 ? have : have >> (seg * LANES) & ((1ull << (LANES & 63)) - 1);
+            if (l == __ffsll((unsigned long long)mine) - 1) {
+                int at = 0;
+                float x = 0.0f;
+#pragma unroll
+                for (int e = EPL - 1; e >= 0; --e)
+                    if (key[e] == most) { at = e; x = v[e]; }
+#pragma unroll
+                for (int e = 0; e < EPL; ++e)
+                    if (e == at) key[e] = KEY_OUT;
+                ids[j] = l * EPL + at;
+                ls[j] = x;
+            }
+        }
+        if (SCORED) {
+            uint64_t again = __ballot(unsure);
+            while (again) {
+                const int s = (__ffsll((unsigned long long)again) - 1) / LANES;
+                again &= LANES == 64 ? 0 : ~(((1ull << (LANES & 63)) - 1) << (s * LANES));
+                const int64_t r = min(row0 + s, p.d.T - 1);
+                choose_in_64_bits<L>(p.d, (const L *)p.logits + r * p.d.ld, p.bias, big[wave], big[wave] + RTP_ROUTE_MAX_EXPERTS,
+                                     slot_id[wave] + s * k, slot_l[wave] + s * k);
+            }
+        }
+        wave_fence();
+        if (row0 + seg < p.d.T) {
+            // renormalised: a softmax over the chosen logits, or over log sigmoid of them (what the sum over all experts or a tiny sigmoid
+            // would divide by cancels)
+            float m = -INFINITY, z = 0.0f;
             if (p.d.renormalise) {
-                // softmax over the chosen logits, or over log sigmoid of them: what the sum over all experts or a tiny
-                // sigmoid would divide by cancels
-                float m = -INFINITY, z = 0.0f;
-                for (int j = 0; j < k; ++j) {
-                    const float o = softmax ? slot_l[w][j] : log_sigmoid(slot_l[w][j]);
-                    m = fmaxf(m, o);
-                }
+                for (int j = 0; j < k; ++j) m = fmaxf(m, softmax ? ls[j] : log_sigmoid(ls[j]));
                 if (m == -INFINITY) m = 0.0f;
-                for (int j = 0; j < k; ++j) {
-                    const float o = softmax ? slot_l[w][j] : log_sigmoid(slot_l[w][j]);
-                    z += slot_l[w][j] == -INFINITY ? 0.0f : expf(o - m);
-                }
-                s = v == -INFINITY ? 0.0f : expf((softmax ? v : log_sigmoid(v)) - m) / z;
-            } else {
-                s = v == -INFINITY ? 0.0f : slot_s[w][lane];
+                for (int j = 0; j < k; ++j) z += ls[j] == -INFINITY ? 0.0f : expf((softmax ? ls[j] : log_sigmoid(ls[j])) - m);
             }
-            p.ids[row * k + lane] = slot_id[w][lane];
-            p.weights[row * k + lane] = p.d.scale * s;
+            for (int j = l; j < k; j += LANES) {
+                const float x = ls[j];
+                float s = p.d.renormalise ? expf((softmax ? x : log_sigmoid(x)) - m) / z : softmax ? expf(x - top) / sum : 1.0f / (1.0f + expf(-x));
+                if (x == -INFINITY) s = 0.0f;
+                p.ids[row * k + j] = ids[j];
+                p.weights[row * k + j] = p.d.scale * s;
+            }
         }
-        __syncthreads();
+        wave_fence();
     }
 }
 
@@ -217,15 +401,29 @@ static hipError_t by_type(rtp_dtype t, F f)
     return f.template operator()<RTP_F16>();
 }
 
-static unsigned route_grid(int64_t T) { return (unsigned)std::min<int64_t>((T + RW - 1) / RW, 1 << 20); }
+static unsigned route_grid(int64_t T, int rows = 1) { return (unsigned)std::min<int64_t>((T + RW * rows - 1) / (RW * rows), 1 << 20); }
 
 struct RouteFwd {
     const RouteArgs &p;
     hipStream_t s;
+    template <rtp_dtype DT, int LANES, int EPL> hipError_t launch()
+    {
+        const unsigned grid = route_grid(p.d.T, 64 / LANES);
+        if (p.bias || p.d.groups > 1) route_fwd_kernel<DT, LANES, EPL, true><<<grid, 64 * RW, 0, s>>>(p);
+        else route_fwd_kernel<DT, LANES, EPL, false><<<grid, 64 * RW, 0, s>>>(p);
+        return hipGetLastError();
+    }
     template <rtp_dtype DT> hipError_t operator()()
     {
-        route_fwd_wave_kernel<DT><<<route_grid(p.d.T), 64 * RW, 0, s>>>(p);
-        return hipGetLastError();
+        // eight experts a lane, sixteen where 64 lanes are not enough
+        if (p.d.E <= 8) return launch<DT, 1, 8>();
+        if (p.d.E <= 16) return launch<DT, 2, 8>();
+        if (p.d.E <= 32) return launch<DT, 4, 8>();
+        if (p.d.E <= 64) return launch<DT, 8, 8>();
+        if (p.d.E <= 128) return launch<DT, 16, 8>();
+        if (p.d.E <= 256) return launch<DT, 32, 8>();
+        if (p.d.E <= 512) return launch<DT, 64, 8>();
+        return launch<DT, 64, 16>();
     }
 };
 
