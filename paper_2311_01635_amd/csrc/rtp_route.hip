@@ -79,83 +79,120 @@ __device__ __forceinline__ float value_of(uint32_t key) { return __uint_as_float
 // The same order as finite doubles.  Beside a NaN logit every softmax is NaN: such choices are alike.
 constexpr double ROW_OUT = -4e300, ROW_CLOSED = -1e300, ROW_NAN = 1e300;
 
+// f over the wave, in every lane
+template <class F> __device__ __forceinline__ double over_wave(double v, F f)
+{
+    uint32_t lo = (uint32_t)__double2loint(v), hi = (uint32_t)__double2hiint(v);
+    auto step = [&](uint32_t l, uint32_t h) {
+        const double r = f(__hiloint2double((int)hi, (int)lo), __hiloint2double((int)h, (int)l));
+        lo = (uint32_t)__double2loint(r);
+        hi = (uint32_t)__double2hiint(r);
+    };
+    step(dpp<DPP_XOR1>(lo), dpp<DPP_XOR1>(hi));
+    step(dpp<DPP_XOR2>(lo), dpp<DPP_XOR2>(hi));
+    step(dpp<DPP_HALF_MIRROR>(lo), dpp<DPP_HALF_MIRROR>(hi));
+    step(dpp<DPP_MIRROR>(lo), dpp<DPP_MIRROR>(hi));
+#pragma unroll
+    for (int half = 16; half <= 32; half *= 2) {
+        const auto l = half == 16 ? __builtin_amdgcn_permlane16_swap(lo, lo, false, false) : __builtin_amdgcn_permlane32_swap(lo, lo, false, false);
+        const auto h = half == 16 ? __builtin_amdgcn_permlane16_swap(hi, hi, false, false) : __builtin_amdgcn_permlane32_swap(hi, hi, false, false);
+        lo = (uint32_t)l[0];
+        hi = (uint32_t)h[0];
+        step((uint32_t)l[1], (uint32_t)h[1]);
+    }
+    return __hiloint2double((int)hi, (int)lo);
+}
 __device__ __forceinline__ double wave_max(double v)
 {
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v = fmax(v, __shfl_xor(v, o));
-    return v;
-}
-__device__ __forceinline__ double wave_add(double v)
-{
-#pragma unroll
-    for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o);
-    return v;
+    return over_wave(v, [](double a, double b) { return fmax(a, b); });
 }
 
-template <class L>
-__device__ __forceinline__ void choose_in_64_bits(const rtp_route_desc &d, const L *l, const float *bias, double *key, double *group, int *slot_id, float *slot_l)
+// EACH: experts of a lane, neighbours, in registers.  (`key` and `group`: LDS, for groups alone.)
+template <int EACH, class L>
+__device__ __forceinline__ void choose_in_64_bits(const rtp_route_desc &d, const L *l, const float *bias, double *key, double *group, int *slot_id)
 {
-    const int lane = threadIdx.x & 63, E = d.E, G = d.groups, len = E / G;
+    const int lane = threadIdx.x & 63, E = d.E, G = d.groups, first = lane * EACH;
     const bool softmax = d.score == RTP_SCORE_SOFTMAX;
+    double v[EACH], c[EACH], add[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        v[e] = first + e < E ? (double)(float)l[first + e] : -INFINITY;
+        add[e] = bias && first + e < E ? (double)bias[first + e] : 0.0;
+    }
     double top = -INFINITY, sum = 0.0;
     if (softmax) {
         bool nan = false;
-        for (int e = lane; e < E; e += 64) {
-            const double v = (double)(float)l[e];
-            nan |= v != v;
-            top = fmax(top, v);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) {
+            nan |= v[e] != v[e];
+            top = fmax(top, v[e]);
         }
         top = wave_max(top);
         if (__any(nan)) top = NAN;
         if (top == -INFINITY) top = 0.0;
-        for (int e = lane; e < E; e += 64) sum += exp((double)(float)l[e] - top);
-        sum = wave_add(sum);
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) sum += exp(v[e] - top);
+        sum = over_wave(sum, [](double a, double b) { return a + b; });
     }
-    wave_fence();
-    for (int e = lane; e < E; e += 64) {
-        const double v = (double)(float)l[e];
-        const double c = v == -INFINITY ? v : (softmax ? exp(v - top) / sum : 1.0 / (1.0 + exp(-v))) + (bias ? (double)bias[e] : 0.0);
-        key[e] = v != v ? ROW_NAN : c != c ? 0.0 : fmin(fmax(c, ROW_CLOSED), 0.5 * ROW_NAN);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+        c[e] = v[e] == -INFINITY ? v[e] : (softmax ? exp(v[e] - top) / sum : 1.0 / (1.0 + exp(-v[e]))) + add[e];
+        c[e] = v[e] != v[e] ? ROW_NAN : c[e] != c[e] ? 0.0 : fmin(fmax(c[e], ROW_CLOSED), 0.5 * ROW_NAN);
+        if (first + e >= E) c[e] = ROW_OUT;
     }
-    wave_fence();
     if (G > 1) {
-        if (lane < G) { // a group's score
-            double a = ROW_OUT, b = ROW_OUT;
-            for (int i = 0; i < len; ++i) {
-                const double v = key[lane * len + i];
-                b = fmax(b, fmin(a, v));
-                a = fmax(a, v);
+        const int len = E / G;
+        wave_fence();
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (first + e < E) key[first + e] = c[e];
+        wave_fence();
+        int S = 64; // lanes to a group
+        while (S * G > 64) S >>= 1;
+        const int g = lane / S;
+        double a = ROW_OUT, b = ROW_OUT;
+        if (g < G) {
+#pragma unroll 4
+            for (int i = lane % S; i < len; i += S) {
+                const double x = key[g * len + i];
+                b = fmax(b, fmin(a, x));
+                a = fmax(a, x);
             }
-            group[lane] = d.group_top == 2 && b > ROW_CLOSED ? a + b : a;
         }
-        wave_fence();
-        for (int g = 0; g < G; ++g) {
-            int before = 0;
-            for (int o = 0; o < G; ++o) before += group[o] > group[g] || (group[o] == group[g] && o < g);
-            if (before >= d.kept_groups)
-                for (int i = lane; i < len; i += 64) key[g * len + i] = ROW_OUT;
+        for (int o = 1; o < S; o <<= 1) {
+            const double x = __shfl_xor(a, o), y = __shfl_xor(b, o);
+            b = fmax(fmax(b, y), fmin(a, x));
+            a = fmax(a, x);
         }
+        if (d.group_top == 2 && b > ROW_CLOSED) a += b;
+        if (g < G && lane % S == 0) group[g] = a;
         wave_fence();
+        int before = 0;
+#pragma unroll 4
+        for (int o = 0; o < G; ++o) before += group[o] > a || (group[o] == a && o < g);
+        if (g < G && before >= d.kept_groups)
+            for (int i = lane % S; i < len; i += S) key[g * len + i] = ROW_OUT;
+        wave_fence();
+#pragma unroll
+        for (int e = 0; e < EACH; ++e)
+            if (first + e < E) c[e] = key[first + e];
     }
     for (int j = 0; j < d.k; ++j) {
-        double best = ROW_OUT;
-        int at = E;
-        for (int e = lane; e < E; e += 64)
-            if (key[e] > best) { best = key[e]; at = e; }
+        double best = c[0];
+        int at = 0;
 #pragma unroll
-        for (int o = 32; o; o >>= 1) {
-            const double b = __shfl_xor(best, o);
-            const int a = __shfl_xor(at, o);
-            if (b > best || (b == best && a < at)) { best = b; at = a; }
+        for (int e = 1; e < EACH; ++e)
+            if (c[e] > best) { best = c[e]; at = e; }
+        // (a lane's experts are neighbours: the lowest lane has the lowest index)
+        const double most = wave_max(best);
+        if (lane == __ffsll((unsigned long long)__ballot(best == most)) - 1) {
+            slot_id[j] = first + at;
+#pragma unroll
+            for (int e = 0; e < EACH; ++e)
+                if (e == at) c[e] = ROW_OUT;
         }
-        wave_fence();
-        if (lane == 0) {
-            slot_id[j] = at;
-            slot_l[j] = (float)l[at];
-            key[at] = ROW_OUT;
-        }
-        wave_fence();
     }
+    wave_fence();
 }
 
 // SCORED: the choice is of scores.  EPL: experts of a lane.
@@ -167,12 +204,12 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
     // a wave's keys in 64 bits and group scores, or its rows' in 32 bits
     __shared__ double big[SCORED ? RW : 1][SCORED ? RTP_ROUTE_MAX_EXPERTS + RTP_ROUTE_MAX_GROUPS : 1];
     __shared__ int slot_id[RW][SLOTS];
-    __shared__ float slot_l[RW][SLOTS];
+    __shared__ float slot_s[RW][SLOTS];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, seg = lane / LANES, l = lane % LANES;
     const int E = p.d.E, k = p.d.k, G = p.d.groups, len = E / G;
     const bool softmax = p.d.score == RTP_SCORE_SOFTMAX;
     int *const ids = slot_id[wave] + seg * k;
-    float *const ls = slot_l[wave] + seg * k;
+    float *const ss = slot_s[wave] + seg * k;
     const int left = E - l * EPL; // of this lane's experts that there are
     for (int64_t row0 = ((int64_t)blockIdx.x * RW + wave) * ROWS; row0 < p.d.T; row0 += (int64_t)gridDim.x * RW * ROWS) {
         const int64_t row = min(row0 + seg, p.d.T - 1);
@@ -199,15 +236,26 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
         }
         uint32_t key[EPL];
         bool unsure = false;
+        // Two numbers closer than `near` of themselves, or than `close`, may be in the other order.  A sigmoid is off by 2.5 2^-23 of
+        // itself (exponential, sum, reciprocal), a softmax by as much, by |l - top| 2^-24, and by its sum, which is the same for all
+        // of a row: 22 roundings for 1024 terms.  A key loses its EPL lowest values to the place, up to EPL - 1 steps of 2^-23 of
+        // itself, and a sum with a bias half a step; of two of them, twice that.
+        const float score = softmax ? 0x1p-17f : 0x1p-20f, near = score + EPL * 0x1p-21f;
+        float close = softmax ? 0x1p-90f : 0x1p-126f; // (a smaller exponential is off by more)
         if (SCORED) {
-            const float inv = 1.0f / sum;
+            const float inv = softmax ? 1.0f / sum : 1.0f;
+            float most = 0.0f;
 #pragma unroll
             for (int e = 0; e < EPL; ++e) {
                 const float b = p.bias && e < left ? p.bias[l * EPL + e] : 0.0f;
-                const float c = (softmax ? expf(v[e] - top) * inv : 1.0f / (1.0f + expf(-v[e]))) + b;
-                unsure |= e < left && (!(fabsf(c) < INFINITY) || v[e] == INFINITY) && v[e] != -INFINITY;
-                key[e] = v[e] == -INFINITY ? KEY_CLOSED : key_of(c);
+                const float x = softmax ? expf(v[e] - top) * inv : __builtin_amdgcn_rcpf(1.0f + expf(-v[e]));
+                const float c = v[e] == -INFINITY ? 0.0f : x + b;
+                unsure |= !(fabsf(c) < INFINITY);
+                most = fmaxf(most, fabsf(c));
+                // the place in the low bits tells a lane's keys apart: the first of equal ones is the largest
+                key[e] = v[e] == -INFINITY ? KEY_CLOSED : (key_of(c) & ~(EPL - 1u)) + (EPL - 1 - e);
             }
+            if (p.bias) close = score * inv + EPL * 0x1p-21f * over_fmax<LANES>(most);
         } else {
 #pragma unroll
             for (int e = 0; e < EPL; ++e) key[e] = key_of(v[e]);
@@ -215,18 +263,7 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
 #pragma unroll
         for (int e = 0; e < EPL; ++e)
             if (e >= left) key[e] = KEY_OUT;
-        // Two numbers closer than this may be in the other order.  A score is off by 2^-19 of itself at most (the 22 roundings of a
-        // sum of 1024 terms, the exponential and the quotient 3 more, and by a denormal), a choice by half a step of the row's largest
-        // on top: four times that.
-        float close = 0x1p-126f;
-        if (SCORED && p.bias) {
-            float most = 0.0f;
-#pragma unroll
-            for (int e = 0; e < EPL; ++e)
-                if (key[e] > KEY_CLOSED) most = fmaxf(most, fabsf(value_of(key[e])));
-            close = 0x1p-17f * (softmax ? 1.0f / sum : 1.0f) + 0x1p-22f * over_fmax<LANES>(most);
-        }
-        auto apart = [&](float a) { return p.bias ? close : 0x1p-17f * a + close; };
+        auto apart = [&](float a) { return p.bias ? close : near * a + close; };
         if (SCORED && G > 1) {
             uint32_t *const keys = (uint32_t *)big[wave] + seg * E;
             float *const group = (float *)(big[wave] + RTP_ROUTE_MAX_EXPERTS / 2) + seg * G;
@@ -264,9 +301,15 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
                 for (int o = 0; o < G; ++o) {
                     const float other = group[o];
                     before += other > mine || (other == mine && o < g);
-                    unsure |= o != g && mine > -INFINITY && fabsf(other - mine) < 2.0f * apart(mine);
                 }
-                if (before >= p.d.kept_groups)
+                const bool out = before >= p.d.kept_groups;
+                // (which of two kept groups is the better one does not matter: only one that is out, and as good as one that is not)
+                if (out && mine > -INFINITY) {
+                    int better = 0; // by more than what may be in the other order
+                    for (int o = 0; o < G; ++o) better += group[o] - mine >= 2.0f * apart(mine);
+                    unsure |= better < p.d.kept_groups;
+                }
+                if (out)
                     for (int i = l % S; i < len; i += S) keys[g * len + i] = KEY_OUT;
             }
             wave_fence();
@@ -290,15 +333,13 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
             const uint64_t mine = LANES == 64 ? have : have >> (seg * LANES) & ((1ull << (LANES & 63)) - 1);
             if (l == __ffsll((unsigned long long)mine) - 1) {
                 int at = 0;
-                float x = 0.0f;
 #pragma unroll
                 for (int e = EPL - 1; e >= 0; --e)
-                    if (key[e] == most) { at = e; x = v[e]; }
+                    if (key[e] == most) at = e;
 #pragma unroll
                 for (int e = 0; e < EPL; ++e)
                     if (e == at) key[e] = KEY_OUT;
                 ids[j] = l * EPL + at;
-                ls[j] = x;
             }
         }
         if (SCORED) {
@@ -307,26 +348,50 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
                 const int s = (__ffsll((unsigned long long)again) - 1) / LANES;
                 again &= LANES == 64 ? 0 : ~(((1ull << (LANES & 63)) - 1) << (s * LANES));
                 const int64_t r = min(row0 + s, p.d.T - 1);
-                choose_in_64_bits<L>(p.d, (const L *)p.logits + r * p.d.ld, p.bias, big[wave], big[wave] + RTP_ROUTE_MAX_EXPERTS,
-                                     slot_id[wave] + s * k, slot_l[wave] + s * k);
+                choose_in_64_bits<(LANES * EPL + 63) / 64>(p.d, (const L *)p.logits + r * p.d.ld, p.bias, big[wave], big[wave] + RTP_ROUTE_MAX_EXPERTS, slot_id[wave] + s * k);
             }
         }
         wave_fence();
-        if (row0 + seg < p.d.T) {
-            // renormalised: a softmax over the chosen logits, or over log sigmoid of them (what the sum over all experts or a tiny sigmoid
-            // would divide by cancels)
-            float m = -INFINITY, z = 0.0f;
+        // weights: lane l has slots l, l + LANES, ..., and all of a row's lanes see its k numbers in LDS
+        auto exchange = [&](auto number) {
+            wave_fence();
+            for (int j = l; j < k; j += LANES) ss[j] = number((float)logits[ids[j]]);
+            wave_fence();
+        };
+        auto total = [&]() {
+            float z = 0.0f;
+            for (int j = 0; j < k; ++j) z += ss[j];
+            return z;
+        };
+        // (a softmax over the chosen: what the sum over all experts, or a sigmoid that underflows, would divide by cancels)
+        auto relative = [&](auto log_of) {
+            float m = -INFINITY;
+            exchange(log_of);
+            for (int j = 0; j < k; ++j) m = fmaxf(m, ss[j]);
+            if (m == -INFINITY) m = 0.0f;
+            exchange([&](float x) { return x == -INFINITY ? 0.0f : expf(log_of(x) - m); });
+        };
+        auto sigmoid = [](float x) { return 1.0f / (1.0f + expf(-x)); };
+        float z = 1.0f;
+        if (softmax && p.d.renormalise) {
+            relative([](float x) { return x; });
+            z = total();
+        } else if (softmax) {
+            exchange([&](float x) { return x == -INFINITY ? 0.0f : expf(x - top) / sum; });
+        } else {
+            exchange(sigmoid);
             if (p.d.renormalise) {
-                for (int j = 0; j < k; ++j) m = fmaxf(m, softmax ? ls[j] : log_sigmoid(ls[j]));
-                if (m == -INFINITY) m = 0.0f;
-                for (int j = 0; j < k; ++j) z += ls[j] == -INFINITY ? 0.0f : expf((softmax ? ls[j] : log_sigmoid(ls[j])) - m);
+                z = total();
+                if (z < 0x1p-100f) { // sigmoids that lose bits, or vanish: from their logarithms
+                    relative(log_sigmoid);
+                    z = total();
+                }
             }
+        }
+        if (row0 + seg < p.d.T) {
             for (int j = l; j < k; j += LANES) {
-                const float x = ls[j];
-                float s = p.d.renormalise ? expf((softmax ? x : log_sigmoid(x)) - m) / z : softmax ? expf(x - top) / sum : 1.0f / (1.0f + expf(-x));
-                if (x == -INFINITY) s = 0.0f;
                 p.ids[row * k + j] = ids[j];
-                p.weights[row * k + j] = p.d.scale * s;
+                p.weights[row * k + j] = p.d.scale * (ss[j] == 0.0f ? 0.0f : ss[j] / z);
             }
         }
         wave_fence();
