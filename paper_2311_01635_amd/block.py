@@ -12,45 +12,64 @@ import torch
 from . import binding as B
 
 _RTP_DT = {torch.float32: B.RTP_F32, torch.bfloat16: B.RTP_BF16, torch.float16: B.RTP_F16}
+_route_fwd, _route_bwd = B.lib.rtp_route_fwd, B.lib.rtp_route_bwd
+_combine_fwd, _combine_bwd = B.lib.rtp_combine_fwd, B.lib.rtp_combine_bwd
+_norm_fwd, _norm_bwd = B.lib.rtp_norm_fwd, B.lib.rtp_norm_bwd
 
 
 def _rows(t, name, dtype, T, cols, dev):
     """Address and leading dimension of a [T, cols] matrix of `dtype` on `dev`, whose rows are contiguous."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 2 or t.dtype != dtype or t.device != dev or t.shape != (T, cols):
-        raise ValueError(f"{name} must be a [{T}, {cols}] tensor of {dtype} on {dev}")
-    ld = t.stride(0)
-    if T <= 1 or ld == cols:
-        ld = cols
-    if (cols > 1 and t.stride(1) != 1) or ld < cols:
-        raise ValueError(f"{name} must have contiguous rows that do not overlap")
-    return t.data_ptr(), ld
+    try:
+        if t.dtype is dtype and t.device == dev and t.shape == (T, cols):
+            if t.is_contiguous():
+                return t.data_ptr(), cols
+            ld, step = t.stride()
+            if T <= 1:
+                ld = max(ld, cols)
+            if ld >= cols and (step == 1 or cols == 1):
+                return t.data_ptr(), ld
+            raise ValueError(f"{name} must have contiguous rows that do not overlap")
+    except AttributeError:       # no tensor
+        pass
+    raise ValueError(f"{name} must be a [{T}, {cols}] tensor of {dtype} on {dev}")
 
 
 def _whole(t, name, dtype, shape, dev):
     """Address of a contiguous tensor."""
-    if not isinstance(t, torch.Tensor) or t.dtype != dtype or t.device != dev or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {dtype} on {dev}")
-    return t.data_ptr()
+    try:
+        if t.dtype is dtype and t.device == dev and t.shape == shape and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of {dtype} on {dev}")
 
 
 def _gpu(t, name):
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a tensor on the GPU")
     return t.device
 
 
 def _float_type(t, name):
-    if t.dtype not in _RTP_DT:
+    code = _RTP_DT.get(t.dtype)
+    if code is None:
         raise ValueError(f"{name} must be float32, bfloat16 or float16")
-    return _RTP_DT[t.dtype]
+    return code
+
+
+# (what torch.cuda.current_device() and current_stream() look up, without the objects they make of it: 3 us a call)
+_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
 
 
 def _call(fn, where, dev, *args):
     """fn(*args, stream) on the caller's current stream of `dev`."""
-    if torch.cuda.current_device() != dev.index:
+    if _device() != dev.index:
         with torch.cuda.device(dev):
-            return B.check(fn(*args, torch.cuda.current_stream(dev).cuda_stream), where)
-    B.check(fn(*args, torch.cuda.current_stream(dev).cuda_stream), where)
+            status = fn(*args, _raw_stream(dev.index))
+    else:
+        status = fn(*args, _raw_stream(dev.index))
+    if status:
+        raise B.RtpError(status, where)
 
 
 class RtpRouter:
@@ -70,31 +89,31 @@ class RtpRouter:
     def forward(self, logits, ids, weights):
         """logits [T, experts] -> ids int32 [T, top_k] (what RtpMoe takes as its route), weights fp32 [T, top_k]."""
         dev = _gpu(logits, "logits")
-        d = self._desc(logits, dev)
-        shape = (logits.shape[0], d.k)
+        d, logits_p = self._desc(logits, dev)
+        shape = (d.T, d.k)
         ids_p, w_p = _whole(ids, "ids", torch.int32, shape, dev), _whole(weights, "weights", torch.float32, shape, dev)
         bias = None if self.bias is None else _whole(self.bias, "bias", torch.float32, (d.E,), dev)
-        _call(B.lib.rtp_route_fwd, "rtp_route_fwd", dev, C.byref(d), logits.data_ptr(), bias, ids_p, w_p)
+        _call(_route_fwd, "rtp_route_fwd", dev, C.byref(d), logits_p, bias, ids_p, w_p)
 
     def backward(self, logits, ids, dweights, dlogits):
         """Gradient of the weights -> that of the logits (in the type of `dlogits`), for the ids of forward()."""
         dev = _gpu(logits, "logits")
-        d = self._desc(logits, dev)
-        shape = (logits.shape[0], d.k)
+        d, logits_p = self._desc(logits, dev)
+        shape = (d.T, d.k)
         ids_p, dw_p = _whole(ids, "ids", torch.int32, shape, dev), _whole(dweights, "dweights", torch.float32, shape, dev)
         if not isinstance(dlogits, torch.Tensor):
             raise ValueError("dlogits must be a tensor")
         d.grad_dtype = _float_type(dlogits, "dlogits")
-        dl_p, d.ld_grad = _rows(dlogits, "dlogits", dlogits.dtype, logits.shape[0], d.E, dev)
-        _call(B.lib.rtp_route_bwd, "rtp_route_bwd", dev, C.byref(d), logits.data_ptr(), ids_p, dw_p, dl_p)
+        dl_p, d.ld_grad = _rows(dlogits, "dlogits", dlogits.dtype, d.T, d.E, dev)
+        _call(_route_bwd, "rtp_route_bwd", dev, C.byref(d), logits_p, ids_p, dw_p, dl_p)
 
     def _desc(self, logits, dev):
         d = B.rtp_route_desc.from_buffer_copy(self.desc)      # (two threads may share a router)
         if logits.dim() != 2:
             raise ValueError("logits must be [tokens, experts]")
         d.dtype, d.T = _float_type(logits, "logits"), logits.shape[0]
-        d.ld = _rows(logits, "logits", logits.dtype, d.T, d.E, dev)[1]
-        return d
+        p, d.ld = _rows(logits, "logits", logits.dtype, d.T, d.E, dev)
+        return d, p
 
 
 class RtpCombine:
@@ -111,7 +130,7 @@ class RtpCombine:
         T, D = self._tokens(Y, "Y")
         yk, ld_yk = _rows(Yk, "Yk", Y.dtype, T * self.k, D, dev)
         y, ld_y = _rows(Y, "Y", Y.dtype, T, D, dev)
-        _call(B.lib.rtp_combine_fwd, "rtp_combine_fwd", dev, T, self.k, D, _float_type(Y, "Y"), yk, ld_yk, self._weights(weights, T, dev), y, ld_y)
+        _call(_combine_fwd, "rtp_combine_fwd", dev, T, self.k, D, _float_type(Y, "Y"), yk, ld_yk, self._weights(weights, T, dev), y, ld_y)
 
     def backward(self, dY, Yk, weights, dYk, dweights=None):
         """dYk = weight * dY and, where asked for, dweights = <dY, Yk>.  (Yk may be None without dweights.)"""
@@ -121,7 +140,7 @@ class RtpCombine:
         yk, ld_yk = (None, 0) if Yk is None else _rows(Yk, "Yk", dY.dtype, T * self.k, D, dev)
         dyk, ld_dyk = (None, 0) if dYk is None else _rows(dYk, "dYk", dY.dtype, T * self.k, D, dev)
         dw = None if dweights is None else _whole(dweights, "dweights", torch.float32, (T, self.k), dev)
-        _call(B.lib.rtp_combine_bwd, "rtp_combine_bwd", dev, T, self.k, D, _float_type(dY, "dY"), dy, ld_dy, yk, ld_yk,
+        _call(_combine_bwd, "rtp_combine_bwd", dev, T, self.k, D, _float_type(dY, "dY"), dy, ld_dy, yk, ld_yk,
               self._weights(weights, T, dev), dyk, ld_dyk, dw)
 
     def expand(self, X, Xk):
@@ -136,6 +155,9 @@ class RtpCombine:
         if t.dim() != 2:
             raise ValueError(f"{name} must be [tokens, width]")
         return t.shape
+
+
+_NONE = (None, 0)
 
 
 class RtpNorm:
@@ -170,6 +192,9 @@ class RtpNorm:
         d.gate = B.RTP_GATE_NONE if gate is None else B.RTP_GATE_CHANNEL
         self.join, self.post, self.pre, self.D = join, post, pre, D
         self.grads = {n: torch.zeros_like(t) for n, t in self.params.items()}
+        at = {n: t.data_ptr() for n, t in self.grads.items()}
+        self._dparams, self._dgate = [at.get(n) for n in self._NAMES[:4]], at.get("gate")
+        self._ws = (-1, 0)                                    # tokens, and the workspace they need
         B.check(B.lib.rtp_norm_fwd(C.byref(d), C.byref(B.rtp_norm_io()), None), "rtp_norm_fwd")     # T = 0: the checks alone
 
     def forward(self, x, y, r, h, stats, gate=None):
@@ -177,16 +202,13 @@ class RtpNorm:
         dev = self._dev(x, "x")
         T = x.shape[0]
         d = self._desc(T, gate, dev)
-        io = B.rtp_norm_io()
-        io.x_dev, io.ld_x = _rows(x, "x", self.stream_dtype, T, self.D, dev)
-        if self.join:
-            io.y_dev, io.ld_y = _rows(y, "y", self.dtype, T, self.D, dev)
-            io.r_dev, io.ld_r = _rows(r, "r", self.stream_dtype, T, self.D, dev)
-        if self.pre:
-            io.h_dev, io.ld_h = _rows(h, "h", self.dtype, T, self.D, dev)
-        if self.pre or self.post:
-            io.stats_dev = _whole(stats, "stats", torch.float32, (T, 4), dev)
-        _call(B.lib.rtp_norm_fwd, "rtp_norm_fwd", dev, C.byref(d), C.byref(io))
+        S, U, D = self.stream_dtype, self.dtype, self.D
+        x_p, ld_x = _rows(x, "x", S, T, D, dev)
+        y_p, ld_y = _rows(y, "y", U, T, D, dev) if self.join else _NONE
+        r_p, ld_r = _rows(r, "r", S, T, D, dev) if self.join else _NONE
+        h_p, ld_h = _rows(h, "h", U, T, D, dev) if self.pre else _NONE
+        st_p = _whole(stats, "stats", torch.float32, (T, 4), dev) if self.pre or self.post else None
+        _call(_norm_fwd, "rtp_norm_fwd", dev, C.byref(d), C.byref(B.rtp_norm_io(x_p, y_p, r_p, h_p, st_p, ld_x, ld_y, ld_r, ld_h)))
 
     def backward(self, r, y, dr, dh, dx, dy, stats, gate=None, dgate=None, accumulate=True):
         """dr (None: nothing follows), dh -> dx, dy, and the parameters' gradients, which it returns (the object's own fp32 tensors;
@@ -194,33 +216,28 @@ class RtpNorm:
         dev = self._dev(dx, "dx")
         T = dx.shape[0]
         d = self._desc(T, gate, dev)
-        g = B.rtp_norm_grads()
-        g.dx_dev, g.ld_dx = _rows(dx, "dx", self.stream_dtype, T, self.D, dev)
-        if dr is not None:
-            g.dr_dev, g.ld_dr = _rows(dr, "dr", self.stream_dtype, T, self.D, dev)
-        if self.pre:
-            g.r_dev, g.ld_r = _rows(r, "r", self.stream_dtype, T, self.D, dev)
-            g.dh_dev, g.ld_dh = _rows(dh, "dh", self.dtype, T, self.D, dev)
-        if self.join:
-            g.dy_dev, g.ld_dy = _rows(dy, "dy", self.dtype, T, self.D, dev)
-        if self.post or d.gate != B.RTP_GATE_NONE:
-            g.y_dev, g.ld_y = _rows(y, "y", self.dtype, T, self.D, dev)
-        if self.pre or self.post:
-            g.stats_dev = _whole(stats, "stats", torch.float32, (T, 4), dev)
-        for n, t in self.grads.items():
-            setattr(g, "dgate_dev" if n == "gate" else f"d{n}_dev", t.data_ptr())
+        S, U, D = self.stream_dtype, self.dtype, self.D
+        dx_p, ld_dx = _rows(dx, "dx", S, T, D, dev)
+        dr_p, ld_dr = _rows(dr, "dr", S, T, D, dev) if dr is not None else _NONE
+        r_p, ld_r = _rows(r, "r", S, T, D, dev) if self.pre else _NONE
+        dh_p, ld_dh = _rows(dh, "dh", U, T, D, dev) if self.pre else _NONE
+        dy_p, ld_dy = _rows(dy, "dy", U, T, D, dev) if self.join else _NONE
+        y_p, ld_y = _rows(y, "y", U, T, D, dev) if self.post or d.gate != B.RTP_GATE_NONE else _NONE
+        st_p = _whole(stats, "stats", torch.float32, (T, 4), dev) if self.pre or self.post else None
+        dg_p, ld_dg = self._dgate, 0
         if dgate is not None:
             if gate is None:
                 raise ValueError("dgate without an element gate")
-            g.dgate_dev, g.ld_dgate = _rows(dgate, "dgate", self.dtype, T, self.D, dev)
-        g.accumulate = int(bool(accumulate))
+            dg_p, ld_dg = _rows(dgate, "dgate", U, T, D, dev)
         ws = None
         if self.grads:
+            if self._ws[0] != T:
+                self._ws = T, B.lib.rtp_norm_ws_bytes(C.byref(d))
             # (a block of torch's allocator: ordered with this stream, and the graph's own while one is captured)
-            g.ws_bytes = B.lib.rtp_norm_ws_bytes(C.byref(d))
-            ws = torch.empty(g.ws_bytes, dtype=torch.uint8, device=dev)
-            g.ws_dev = ws.data_ptr()
-        _call(B.lib.rtp_norm_bwd, "rtp_norm_bwd", dev, C.byref(d), C.byref(g))
+            ws = torch.empty(self._ws[1], dtype=torch.uint8, device=dev)
+        g = B.rtp_norm_grads(r_p, y_p, dr_p, dh_p, st_p, dx_p, dy_p, dg_p, *self._dparams, 1 if accumulate else 0, None if ws is None else ws.data_ptr(),
+                             self._ws[1], ld_r, ld_y, ld_dr, ld_dh, ld_dx, ld_dy, ld_dg)
+        _call(_norm_bwd, "rtp_norm_bwd", dev, C.byref(d), C.byref(g))
         return self.grads
 
     def zero_grads(self):
