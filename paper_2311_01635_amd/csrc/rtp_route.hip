@@ -398,62 +398,104 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
     }
 }
 
-template <rtp_dtype DT, rtp_dtype GT>
-__global__ __launch_bounds__(64 * RW) void route_bwd_wave_kernel(RouteArgs p)
+// Gradient of the logits, rows and lanes as in the forward pass.  Bound: HBM for many tokens (every entry is read and written), latency for
+// few.  With d_j = a_j - sum of w_i a_i / scale: renormalised, dl_j = w_j d_j (softmax), w_j (1 - s_j) d_j (sigmoid), nothing
+// elsewhere; else dl_e = scale p_e ([chosen] a - sum of p_i a_i), scale s (1 - s) a.
+template <rtp_dtype DT, rtp_dtype GT, int LANES, int EPL>
+__global__ __launch_bounds__(64 * RW) void route_bwd_kernel(RouteArgs p)
 {
     using L = typename Elem<DT>::t;
-    using G = typename Elem<GT>::t;
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, E = p.d.E, k = p.d.k;
-    const bool softmax = p.d.score == RTP_SCORE_SOFTMAX;
-    const float scale = p.d.scale;
-    for (int64_t row = (int64_t)blockIdx.x * RW + w; row < p.d.T; row += (int64_t)gridDim.x * RW) {
-        const L *l = (const L *)p.logits + row * p.d.ld;
-        G *out = (G *)p.dlogits + row * p.d.ld_grad;
-        const int32_t *ids = p.ids_in + row * k;
-        const float *a = p.dweights + row * k;
-        auto logit = [&](int j) { // of a slot that has a part in the gradient, else -infinity
-            const int e = ids[j];
-            return (unsigned)e < (unsigned)E ? (float)l[e] : -INFINITY;
-        };
-        auto lg = [&](float v) { return softmax ? v : log_sigmoid(v); };
-        float m = -INFINITY, z = 0.0f, dot = 0.0f;
-        if (p.d.renormalise) { // (NaN: the maximum passes it over, the sums do not)
-            for (int j = 0; j < k; ++j) m = fmaxf(m, lg(logit(j)));
-            if (m == -INFINITY) m = 0.0f;
-            for (int j = 0; j < k; ++j) {
-                const float v = logit(j), x = v == -INFINITY ? 0.0f : expf(lg(v) - m);
-                z += x;
-                dot += x == 0.0f ? 0.0f : x * a[j];
-            }
-            dot /= z > 0.0f ? z : 1.0f;
-        } else if (softmax) {
-            for (int e = lane; e < E; e += 64) m = fmaxf(m, (float)l[e]);
+    constexpr int ROWS = 64 / LANES, SLOTS = ROWS * (LANES * EPL < RTP_ROUTE_MAX_TOP ? LANES * EPL : RTP_ROUTE_MAX_TOP);
+    __shared__ int slot_id[RW][SLOTS];
+    __shared__ float slot_a[RW][SLOTS], slot_x[RW][SLOTS]; // gradient of a slot's weight, its logit
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, seg = lane / LANES, l = lane % LANES;
+    const int E = p.d.E, k = p.d.k;
+    const bool softmax = p.d.score == RTP_SCORE_SOFTMAX, renorm = p.d.renormalise;
+    int *const ids = slot_id[wave] + seg * k;
+    float *const as = slot_a[wave] + seg * k, *const xs = slot_x[wave] + seg * k;
+    const int left = E - l * EPL;
+    for (int64_t row0 = ((int64_t)blockIdx.x * RW + wave) * ROWS; row0 < p.d.T; row0 += (int64_t)gridDim.x * RW * ROWS) {
+        const int64_t row = min(row0 + seg, p.d.T - 1);
+        const L *const logits = (const L *)p.logits + row * p.d.ld;
+        wave_fence();
+        for (int j = l; j < k; j += LANES) {
+            const int e = p.ids_in[row * k + j];
+            const bool there = (unsigned)e < (unsigned)E;
+            const float x = there ? (float)logits[e] : -INFINITY;
+            ids[j] = there ? e : -1;
+            xs[j] = x;
+            as[j] = x == -INFINITY ? 0.0f : p.dweights[row * k + j]; // (closed: whatever came back has no part)
+        }
+        float v[EPL];
 #pragma unroll
-            for (int o = 32; o; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+        for (int i = 0; i < EPL; i += 8) {
+            Eight<DT> x;
+            if (left > i) x.load(logits + l * EPL + i, left - i);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[i + e] = i + e < left ? x.get(e) : -INFINITY;
+        }
+        wave_fence();
+        // maximum and sum of the exponentials that the weights are quotients of (NaN: the maximum passes it over, the sum does not)
+        auto lg = [&](float x) { return softmax ? x : log_sigmoid(x); };
+        float m = -INFINITY, z = 0.0f, dot = 0.0f;
+        if (renorm) {
+            for (int j = 0; j < k; ++j) m = fmaxf(m, lg(xs[j]));
             if (m == -INFINITY) m = 0.0f;
-            for (int e = lane; e < E; e += 64) z += expf((float)l[e] - m);
-            z = wave_sum(z);
             for (int j = 0; j < k; ++j) {
-                const float v = logit(j);
-                dot += v == -INFINITY ? 0.0f : expf(v - m) / z * a[j];
+                const float x = xs[j] == -INFINITY ? 0.0f : expf(lg(xs[j]) - m);
+                z += x;
+                dot += x == 0.0f ? 0.0f : x * as[j];
+            }
+        } else if (softmax) {
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) m = fmaxf(m, v[e]);
+            m = over_fmax<LANES>(m);
+            if (m == -INFINITY) m = 0.0f;
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) z += expf(v[e] - m);
+            z = over_sum<LANES>(z);
+            for (int j = 0; j < k; ++j) dot += xs[j] == -INFINITY ? 0.0f : expf(xs[j] - m) * as[j];
+        }
+        if (z == 0.0f) z = 1.0f;
+        dot /= z;
+        // what the slots that name this lane's experts bring, and how many do
+        float g[EPL], n[EPL];
+#pragma unroll
+        for (int e = 0; e < EPL; ++e) g[e] = n[e] = 0.0f;
+        for (int j = 0; j < k; ++j) {
+            const int at = ids[j] - l * EPL;
+            const float a = as[j];
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) {
+                g[e] += e == at ? a : 0.0f;
+                n[e] += e == at ? 1.0f : 0.0f;
             }
         }
-        for (int e = lane; e < E; e += 64) {
-            const float v = (float)l[e];
-            float g = 0.0f, n = 0.0f; // sum of the slots' gradients, and how many name this expert
-            for (int j = 0; j < k; ++j)
-                if (ids[j] == e) { g += a[j]; n += 1.0f; }
-            float d = 0.0f;
-            if (v != -INFINITY) {
-                const float sig = 1.0f / (1.0f + expf(-v));
-                if (p.d.renormalise)
-                    d = n == 0.0f ? 0.0f : expf(lg(v) - m) / z * (g - n * dot) * (softmax ? 1.0f : 1.0f - sig);
-                else if (softmax)
-                    d = expf(v - m) / z * (g - dot);
-                else
-                    d = n == 0.0f ? 0.0f : sig * (1.0f - sig) * g;
+        if (row0 + seg < p.d.T) {
+            float o[EPL];
+#pragma unroll
+            for (int e = 0; e < EPL; ++e) {
+                float d = 0.0f;
+                const bool open = v[e] != -INFINITY;
+                if (softmax && !renorm) {
+                    d = open ? expf(v[e] - m) / z * (g[e] - dot) : 0.0f;
+                } else if (open && n[e] > 0.0f) {
+                    const float sig = 1.0f / (1.0f + expf(-v[e]));
+                    d = renorm ? expf(lg(v[e]) - m) / z * (g[e] - n[e] * dot) * (softmax ? 1.0f : 1.0f - sig) : sig * (1.0f - sig) * g[e];
+                }
+                o[e] = p.d.scale * d;
             }
-            out[e] = (G)(scale * d);
+            using G = typename Elem<GT>::t;
+#pragma unroll
+            for (int i = 0; i < EPL; i += 8) {
+                if (left <= i) continue;
+                Eight<GT> x;
+                float t[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) t[e] = o[i + e];
+                x.set(t);
+                x.store((G *)p.dlogits + row * p.d.ld_grad + l * EPL + i, left - i);
+            }
         }
     }
 }
@@ -466,29 +508,40 @@ static hipError_t by_type(rtp_dtype t, F f)
     return f.template operator()<RTP_F16>();
 }
 
-static unsigned route_grid(int64_t T, int rows = 1) { return (unsigned)std::min<int64_t>((T + RW * rows - 1) / (RW * rows), 1 << 20); }
+static unsigned route_grid(int64_t T, int rows) { return (unsigned)std::min<int64_t>((T + RW * rows - 1) / (RW * rows), 1 << 20); }
 
-struct RouteFwd {
+// f.launch<LANES, EPL>(): eight experts a lane, sixteen where 64 lanes are not enough
+template <class F>
+static hipError_t by_experts(int E, F &f)
+{
+    if (E <= 8) return f.template launch<1, 8>();
+    if (E <= 16) return f.template launch<2, 8>();
+    if (E <= 32) return f.template launch<4, 8>();
+    if (E <= 64) return f.template launch<8, 8>();
+    if (E <= 128) return f.template launch<16, 8>();
+    if (E <= 256) return f.template launch<32, 8>();
+    if (E <= 512) return f.template launch<64, 8>();
+    return f.template launch<64, 16>();
+}
+
+template <rtp_dtype DT> struct RouteFwdOf {
     const RouteArgs &p;
     hipStream_t s;
-    template <rtp_dtype DT, int LANES, int EPL> hipError_t launch()
+    template <int LANES, int EPL> hipError_t launch()
     {
         const unsigned grid = route_grid(p.d.T, 64 / LANES);
         if (p.bias || p.d.groups > 1) route_fwd_kernel<DT, LANES, EPL, true><<<grid, 64 * RW, 0, s>>>(p);
         else route_fwd_kernel<DT, LANES, EPL, false><<<grid, 64 * RW, 0, s>>>(p);
         return hipGetLastError();
     }
+};
+struct RouteFwd {
+    const RouteArgs &p;
+    hipStream_t s;
     template <rtp_dtype DT> hipError_t operator()()
     {
-        // eight experts a lane, sixteen where 64 lanes are not enough
-        if (p.d.E <= 8) return launch<DT, 1, 8>();
-        if (p.d.E <= 16) return launch<DT, 2, 8>();
-        if (p.d.E <= 32) return launch<DT, 4, 8>();
-        if (p.d.E <= 64) return launch<DT, 8, 8>();
-        if (p.d.E <= 128) return launch<DT, 16, 8>();
-        if (p.d.E <= 256) return launch<DT, 32, 8>();
-        if (p.d.E <= 512) return launch<DT, 64, 8>();
-        return launch<DT, 64, 16>();
+        RouteFwdOf<DT> f{p, s};
+        return by_experts(p.d.E, f);
     }
 };
 
@@ -498,13 +551,22 @@ hipError_t launch_route_fwd(const rtp_route_desc &d, const void *logits, const f
     return by_type(d.dtype, RouteFwd{p, s});
 }
 
+template <rtp_dtype DT, rtp_dtype GT> struct RouteBwdOf {
+    const RouteArgs &p;
+    hipStream_t s;
+    template <int LANES, int EPL> hipError_t launch()
+    {
+        route_bwd_kernel<DT, GT, LANES, EPL><<<route_grid(p.d.T, 64 / LANES), 64 * RW, 0, s>>>(p);
+        return hipGetLastError();
+    }
+};
 template <rtp_dtype DT> struct RouteBwdTo {
     const RouteArgs &p;
     hipStream_t s;
     template <rtp_dtype GT> hipError_t operator()()
     {
-        route_bwd_wave_kernel<DT, GT><<<route_grid(p.d.T), 64 * RW, 0, s>>>(p);
-        return hipGetLastError();
+        RouteBwdOf<DT, GT> f{p, s};
+        return by_experts(p.d.E, f);
     }
 };
 struct RouteBwd {
