@@ -549,8 +549,8 @@ __global__ __launch_bounds__(SUM_THREADS) void norm_sums_kernel(NormSums p)
             for (int b = group; b < p.parts; b += SUM_GROUPS) v += p.ws[((int64_t)b * p.nsums + at) * p.D + i];
         }
         ++at;
-        v += __shfl_xor(v, 16);
-        v += __shfl_xor(v, 32);
+#pragma unroll
+        for (int o = SUM_COLS; o < 64; o *= 2) v += __shfl_xor(v, o);
         if (threadIdx.x % 64 < SUM_COLS) lds[k][threadIdx.x / 64][col] = v;
     }
     __syncthreads();
@@ -626,21 +626,24 @@ hipError_t launch_norm_fwd(const rtp_norm_desc &d, const rtp_norm_io &io, hipStr
     return by_types(d, RunFwd{p, s});
 }
 
-// Workgroups of the backward pass: one to a compute unit, each of which leaves its sums.  (Two: 1990 rows of 768 24.8 us in all instead of
-// 20.4, 8192 of 8192 199 instead of 190.)
+// Workgroups of the backward pass, each of which leaves its sums: one to a compute unit; two where they have eight turns and more
+// and there is room for two (256 threads, a 16-bit stream).  Two for all: 1990 rows of 768 24.8 us instead of 20.4, 8192 of 4096 with an fp32
+// stream 150 instead of 137; one for all: 8192 rows of 2048 80 us instead of 55, of 4096 101 instead of 84.
 struct Parts {
     int64_t T;
+    bool half; // a 16-bit stream
     template <int THREADS, int NV> hipError_t operator()()
     {
         constexpr int BLOCK = norm_block<THREADS>(), ROWS = BLOCK / THREADS;
-        T = std::min<int64_t>((T + ROWS - 1) / ROWS, 256);
+        const int64_t turns = (T + ROWS - 1) / ROWS;
+        T = std::min<int64_t>(turns, BLOCK == 256 && half && turns >= 4096 ? 512 : 256);
         return hipSuccess;
     }
 };
 int norm_bwd_parts(const rtp_norm_desc &d)
 {
     if (d.D > NORM_REG_D) return (int)std::min<int64_t>(d.T, 1024);
-    Parts parts{d.T};
+    Parts parts{d.T, d.stream_dtype != RTP_F32};
     (void)by_length(d.D, parts);
     return (int)parts.T;
 }
