@@ -642,7 +642,7 @@ struct Parts {
 };
 int norm_bwd_parts(const rtp_norm_desc &d)
 {
-    if (d.D > NORM_REG_D) return (int)std::min<int64_t>(d.T, 1024);
+    if (d.D > NORM_REG_D) return (int)std::min<int64_t>(d.T, 512);
     Parts parts{d.T, d.stream_dtype != RTP_F32};
     (void)by_length(d.D, parts);
     return (int)parts.T;

@@ -364,9 +364,13 @@ class RtpMoe(_PassStreams):
         self.yk = self._slots(self.yk, self.O2)
         if k > 1:
             self.xk = self._slots(self.xk, self.I)
-            self.combine.expand(X, self.xk)
-        self._forward(self.xk if k > 1 else X, route, self.yk)
-        self.combine.forward(self.yk, weights, Y)
+        self._enter()
+        with torch.cuda.stream(self.compute_stream):    # (where the slots' rows are read and written by every pass, in order)
+            if k > 1:
+                self.combine.expand(X, self.xk)
+            self._forward(self.xk if k > 1 else X, route, self.yk)
+            self.combine.forward(self.yk, weights, Y)
+        self._leave()
 
     def backward(self, dY, dX, weights=None, dweights=None):
         """weights: those of forward().  dweights (fp32 [T, top_k], or None): their gradient."""
@@ -377,13 +381,15 @@ class RtpMoe(_PassStreams):
         if dweights is not None and self.yk is None:
             raise ValueError("the forward pass had no weights")
         self.gk = self._slots(self.gk, self.O2)
-        self.combine.backward(dY, self.yk if dweights is not None else None, weights, self.gk, dweights)
-        if k == 1:
-            self._backward(self.gk, dX)
-            return
-        self.xk = self._slots(self.xk, self.I)      # (the layer keeps its own grouped copy of the forward pass's rows)
-        self._backward(self.gk, self.xk)
-        self.combine.forward(self.xk, None, dX)
+        if k > 1:
+            self.xk = self._slots(self.xk, self.I)      # (the layer keeps its own grouped copy of the forward pass's rows)
+        self._enter()
+        with torch.cuda.stream(self.compute_stream):
+            self.combine.backward(dY, self.yk if dweights is not None else None, weights, self.gk, dweights)
+            self._backward(self.gk, self.xk if k > 1 else dX)
+            if k > 1:
+                self.combine.forward(self.xk, None, dX)
+        self._leave()
 
     def _slots(self, buf, cols):
         return torch.empty(self.T, cols, dtype=_TORCH_DT[self.dtype], device=self.dev) if buf is None else buf

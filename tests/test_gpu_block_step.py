@@ -111,6 +111,42 @@ def test_moe_without_weights_is_what_it_was():
     assert torch.equal(res[0][0], res[1][0]) and torch.equal(res[0][1], res[1][1])
 
 
+def test_weighted_moe_calls_from_several_streams():
+    """calls that nothing but the layer itself orders (each on a stream of its own, the compute stream held back): the slots' rows of one
+    are not overwritten by the next"""
+    T, I, O, n, k = 64, 128, 128, 4, 2
+    inp = wl.make_moe_inputs(T, I, O, I, n, seed=3)
+    moe = RtpMoe([tuple(_dev(m, BF) for m in ex) for ex in inp["experts"]], T, 0, B.RTP_ACT_GELU_ERF, top_k=k)
+    g = torch.Generator(device=DEV).manual_seed(1)
+    calls = []
+    for _ in range(4):
+        X, dY = (torch.randn(T, I, generator=g, device=DEV).to(BF) for _ in range(2))
+        ids = torch.stack([torch.randperm(n, generator=g, device=DEV)[:k] for _ in range(T)]).int()
+        calls.append((X, dY, ids, torch.rand(T, k, generator=g, device=DEV), [_new(T, I), _new(T, I), _new(T, k, dt=F32)]))
+
+    def run(c):
+        X, dY, ids, w, (Y, dX, dw) = c
+        moe.forward(X, ids, Y, w)
+        moe.backward(dY, dX, w, dw)
+    want = []
+    for c in calls:
+        run(c)
+        moe.sync()
+        want.append([t.clone() for t in c[4]])
+        for t in c[4]:
+            t.fill_(math.nan)
+    scratch = torch.zeros(16, dtype=torch.uint8, device=DEV)
+    B.check(B.lib.rtp_ring_set_test_delay_compute(moe.ring_handle(), scratch.data_ptr(), 100))
+    torch.cuda.synchronize()
+    for c in calls:
+        with torch.cuda.stream(torch.cuda.Stream()):
+            run(c)
+    torch.cuda.synchronize()
+    for c, w in zip(calls, want):
+        assert _same(c[4], w)
+    moe.close()
+
+
 def test_moe_refuses_a_route_of_another_shape():
     T, I, n = 64, 128, 2
     inp = wl.make_moe_inputs(T, I, 128, I, n, seed=3)
