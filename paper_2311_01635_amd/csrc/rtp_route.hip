@@ -238,9 +238,9 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
         bool unsure = false;
         // Two numbers closer than `near` of themselves, or than `close`, may be in the other order.  A sigmoid is off by 2.5 2^-23 of
         // itself (exponential, sum, reciprocal), a softmax by as much, by |l - top| 2^-24, and by its sum, which is the same for all
-        // of a row: 22 roundings for 1024 terms.  A key loses its EPL lowest values to the place, up to EPL - 1 steps of 2^-23 of
-        // itself, and a sum with a bias half a step; of two of them, twice that.
-        const float score = softmax ? 0x1p-17f : 0x1p-20f, near = score + EPL * 0x1p-21f;
+        // of a row: 22 roundings for 1024 terms.  A choice is off by half a step of the row's largest on top; two of them by twice
+        // all that.
+        const float near = softmax ? 0x1p-17f : 0x1p-20f;
         float close = softmax ? 0x1p-90f : 0x1p-126f; // (a smaller exponential is off by more)
         if (SCORED) {
             const float inv = softmax ? 1.0f / sum : 1.0f;
@@ -252,10 +252,9 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
                 const float c = v[e] == -INFINITY ? 0.0f : x + b;
                 unsure |= !(fabsf(c) < INFINITY);
                 most = fmaxf(most, fabsf(c));
-                // the place in the low bits tells a lane's keys apart: the first of equal ones is the largest
-                key[e] = v[e] == -INFINITY ? KEY_CLOSED : (key_of(c) & ~(EPL - 1u)) + (EPL - 1 - e);
+                key[e] = v[e] == -INFINITY ? KEY_CLOSED : key_of(c);
             }
-            if (p.bias) close = score * inv + EPL * 0x1p-21f * over_fmax<LANES>(most);
+            if (p.bias) close = near * inv + 0x1p-22f * over_fmax<LANES>(most);
         } else {
 #pragma unroll
             for (int e = 0; e < EPL; ++e) key[e] = key_of(v[e]);

@@ -118,6 +118,23 @@ def test_near_ties_are_decided_in_64_bits():
     assert ids.cpu().tolist() == [[37, 5, 0]] * 8
 
 
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("biased", [False, True])
+@pytest.mark.parametrize("E,groups", [(32, 4), (256, 8), (600, 6)])
+def test_choices_about_as_close_as_32_bits_can_tell(E, groups, biased, score):
+    """scores and biases that differ by 2^-16 to 2^-26 of themselves, around several sizes: whichever of them the kernel decides in 32 bits, it
+    decides as 64 bits do"""
+    g = torch.Generator().manual_seed(E)
+    T = 96
+    size = torch.tensor([0.0, 1.0, -3.0, 6.0, -20.0, 12.0])[torch.arange(T) % 6][:, None]
+    spread = 2.0 ** -torch.randint(16, 27, (T, 1), generator=g)
+    l = size * (1 + spread * torch.randn(T, E, generator=g)) + spread * torch.randn(T, E, generator=g)
+    bias = 1.0 + 2.0 ** -20 * torch.randn(E, generator=g) if biased else None
+    # (equal logits with equal biases are equal in any arithmetic; others differ by 2^-24 of something, where 64 bits have 2^-52 left)
+    _, ids, _ = _run(l.to(DEV), 6, None if bias is None else bias.to(DEV), score=score, groups=groups, kept=3)
+    assert torch.equal(ids.cpu(), ref.route(l, 6, score=score, groups=groups, kept=3, bias=bias)[0])
+
+
 @pytest.mark.parametrize("gdt", [F32, BF16, F16])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c[:3])))
