@@ -9,8 +9,9 @@ namespace rtp {
 // Bound: HBM, 12 to 30 bytes a parameter that are read and written once.  With 8-bit moments the arithmetic is as long: at 6 TB/s a
 // parameter's 12 bytes leave a compute unit time for 79 instructions a wave, and the hash, the update and two
 // conversions are about 70 of them.  A wave takes four blocks of 256, a lane four neighbours of each: their 16 loads are sent
-// before the first is waited for (past the caches: 762 -> 706 us for 135M with fp32 moments and masters), a block's largest element is a
-// reduction within the wave, and nothing needs a barrier.
+// before the first is waited for (past the caches: 752 -> 706 us for 135M with fp32 moments and masters, 5.7 TB/s), a block's largest
+// element is a reduction within the wave, and nothing needs a barrier.  135M with 8-bit moments: 282 us, 5.8 TB/s; a thread an
+// element, blocks of 256 threads: 1400.
 constexpr int AT = 256, AB = 4; // threads, blocks of a wave
 static_assert(AT / 64 * AB == ADAMW_CHUNK_BLOCKS, "a workgroup is a chunk");
 
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(AT) void adamw_kernel(AdamwArgs p)
 }
 
 // Moments as numbers.  Bound: HBM.  A thread takes eight neighbours, a block 32 threads (16 to a thread left holes of 16 bytes in what a
-// store instruction writes: 285 us instead of 160 for 135M of 8 bits).
+// store instruction writes: 278 us instead of 129 for 135M of 8 bits).
 template <rtp_moments MO, rtp_dtype DT>
 __global__ __launch_bounds__(AT) void adamw_moments_kernel(const void *m, const void *v, const uint8_t *exps, int64_t blocks, void *m_out, void *v_out)
 {

@@ -1,7 +1,8 @@
 // Weighted combination of what a token's k experts give, and its gradients (rtp_combine_fwd, rtp_combine_bwd).
 //
 // Bound: HBM, a fused multiply-add or two an element.  THREADS threads share a token (a wave where that is enough: no barrier) and go
-// along its row eight elements at a time, with the loads of K slots in flight together.  K is the number of slots, rounded up to a
+// along its row eight elements at a time, with the loads of K slots in flight together, past the caches (8192 tokens of 2 x 4096 33 us,
+// 6.1 TB/s; through them 35.5), and those of the weights beside them.  K is the number of slots, rounded up to a
 // power of two, or chunks of 8.
 #include "rtp_block_kernels.h"
 #include "rtp_elem.h"

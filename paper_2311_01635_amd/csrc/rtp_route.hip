@@ -11,6 +11,9 @@ namespace rtp {
 // LANES lanes, and the lowest lane that has it, with no barrier and little LDS.  Keys are 32-bit integers in the order of what they
 // stand for.  Where the choice is of scores (a bias, groups), they are scores in 32 bits; a row in which two of them that
 // matter are closer than 32 bits can tell apart is decided again in 64 bits by its whole wave.
+// 16384 tokens over 256 experts in 8 groups, 8 a token: 30 us (all rows in 64 bits, a wave a row: 117); 23 are the 32-bit choice, of
+// which the groups 4, the rest the few rows in doubt: 4 us each, one after the other, behind the last ones.  Sixteen lanes of
+// sixteen instead of 32 of eight: 34.  8192 over 8, two a token: 4.5 us, latency.
 constexpr int RW = 4; // waves of a workgroup
 
 struct RouteArgs {
@@ -398,7 +401,7 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
 }
 
 // Gradient of the logits, rows and lanes as in the forward pass.  Bound: HBM for many tokens (every entry is read and written), latency for
-// few.  With d_j = a_j - sum of w_i a_i / scale: renormalised, dl_j = w_j d_j (softmax), w_j (1 - s_j) d_j (sigmoid), nothing
+// few (5003 tokens over 150: 7.3 us; a wave a row 9.4).  With d_j = a_j - sum of w_i a_i / scale: renormalised, dl_j = w_j d_j (softmax), w_j (1 - s_j) d_j (sigmoid), nothing
 // elsewhere; else dl_e = scale p_e ([chosen] a - sum of p_i a_i), scale s (1 - s) a.
 template <rtp_dtype DT, rtp_dtype GT, int LANES, int EPL>
 __global__ __launch_bounds__(64 * RW) void route_bwd_kernel(RouteArgs p)
