@@ -335,6 +335,8 @@ class RtpAdamW:
             h = C.byref(self._hyper(lr, step, betas, eps, seed))
         else:
             sc = _whole(scalars, "scalars", torch.uint8, (C.sizeof(B.rtp_adamw_scalars),), self.dev)
+        if grad_scale is not None and not (isinstance(grad_scale, torch.Tensor) and grad_scale.numel() == 1):
+            raise ValueError("grad_scale must be a tensor of one value")
         gs = None if grad_scale is None else _whole(grad_scale.reshape(1), "grad_scale", torch.float32, (1,), self.dev)
         for layer in self.layers:
             layer._enter()

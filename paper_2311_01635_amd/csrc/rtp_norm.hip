@@ -252,7 +252,7 @@ struct NormBwd {
     int nsums;
 };
 
-// Rows in registers.  Bound: HBM.  8192 rows of 8192 (bf16): 143 us and 8 for the sums, 5.4 TB/s; without the next row on its way 186.  1990
+// Rows in registers.  Bound: HBM.  8192 rows of 8192 (bf16): 150 us, 8 of them the sums, 5.4 TB/s; without the next row on its way 190.  1990
 // rows of 768 with every part: 14 and 5 us, latency (two rows a wave, one after the other).  Rows of more than 8192 do not
 // fit 128 registers a thread and spill: 1.2 to 1.7 TB/s.  The sums over rows stay in registers too, a thread's columns over all rows of its workgroup, so
 // that they cost one write a workgroup (and one read by norm_sums_kernel, which adds the workgroups up in a fixed order).

@@ -10,10 +10,11 @@ namespace rtp {
 // a row, eight or sixteen neighbouring experts each, 64 / LANES rows to a wave: a round is then a maximum over a lane's keys, one over
 // LANES lanes, and the lowest lane that has it, with no barrier and little LDS.  Keys are 32-bit integers in the order of what they
 // stand for.  Where the choice is of scores (a bias, groups), they are scores in 32 bits; a row in which two of them that
-// matter are closer than 32 bits can tell apart is decided again in 64 bits by its whole wave.
-// 16384 tokens over 256 experts in 8 groups, 8 a token: 30 us (all rows in 64 bits, a wave a row: 117); 23 are the 32-bit choice, of
-// which the groups 4, the rest the few rows in doubt: 4 us each, one after the other, behind the last ones.  Sixteen lanes of
-// sixteen instead of 32 of eight: 34.  8192 over 8, two a token: 4.5 us, latency.
+// matter are closer than 32 bits can tell apart is decided again in 64 bits: the chosen are put in order among themselves, or, where
+// it is in doubt who they are, the whole wave chooses again.
+// 16384 tokens over 256 experts in 8 groups, 8 a token: 28 us (all rows in 64 bits, a wave a row: 117); 23 are the 32-bit choice, of
+// which the groups 4, the rest the few rows in doubt (0.1 %), behind the last ones: 4 us to choose one again, which all of
+// them did at 30 us.  Sixteen lanes of sixteen instead of 32 of eight: 34.  8192 over 8, two a token: 4.5 us, latency.
 constexpr int RW = 4; // waves of a workgroup
 
 struct RouteArgs {
@@ -238,7 +239,7 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
             sum = over_sum<LANES>(sum);
         }
         uint32_t key[EPL];
-        bool unsure = false;
+        bool unsure = false, disordered = false; // who is chosen, and in which order they are
         // Two numbers closer than `near` of themselves, or than `close`, may be in the other order.  A sigmoid is off by 2.5 2^-23 of
         // itself (exponential, sum, reciprocal), a softmax by as much, by |l - top| 2^-24, and by its sum, which is the same for all
         // of a row: 22 roundings for 1024 terms.  A choice is off by half a step of the row's largest on top; two of them by twice
@@ -326,7 +327,11 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
             for (int e = 0; e < EPL; ++e) best = max(best, key[e]);
             const uint32_t most = over_max<LANES>(best);
             if (SCORED) {
-                if (j > 0 && most > KEY_CLOSED) unsure |= value_of(last) - value_of(most) < apart(value_of(last));
+                if (j > 0 && most > KEY_CLOSED && value_of(last) - value_of(most) < apart(value_of(last))) {
+                    // (the order of a softmax with a bias takes its sum in 64 bits, and that of vanishing ones is of equals)
+                    if (j < k && (softmax ? !p.bias && value_of(most) > 0x1p-80f : true)) disordered = true;
+                    else unsure = true;
+                }
                 last = most;
                 if (j == k) break;
             }
@@ -343,6 +348,24 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
                     if (e == at) key[e] = KEY_OUT;
                 ids[j] = l * EPL + at;
             }
+        }
+        if (SCORED && disordered) { // the chosen among themselves: each counts the better ones
+            double *const c = big[wave] + seg * k;
+            int *const sorted = (int *)ss;
+            wave_fence();
+            for (int j = l; j < k; j += LANES) {
+                const double x = (double)(float)logits[ids[j]];
+                c[j] = x == -INFINITY ? ROW_CLOSED : softmax ? x : 1.0 / (1.0 + exp(-x)) + (p.bias ? (double)p.bias[ids[j]] : 0.0);
+            }
+            wave_fence();
+            for (int j = l; j < k; j += LANES) {
+                int better = 0;
+                for (int o = 0; o < k; ++o) better += c[o] > c[j] || (c[o] == c[j] && ids[o] < ids[j]);
+                sorted[better] = ids[j];
+            }
+            wave_fence();
+            for (int j = l; j < k; j += LANES) ids[j] = sorted[j];
+            wave_fence();
         }
         if (SCORED) {
             uint64_t again = __ballot(unsure);

@@ -279,5 +279,6 @@ def test_refusals_on_the_device():
     for kw in (dict(lr=math.nan, step=1), dict(lr=1e-3, step=0), dict(lr=1e-3, step=1, eps=0.0), dict(lr=1e-3, step=1, betas=(1.0, 0.9))):
         with pytest.raises(B.RtpError):
             opt.step(**kw)
-    with pytest.raises(ValueError):
-        opt.step(1e-3, 1, grad_scale=torch.ones(1))
+    for scale in (torch.ones(1), torch.ones(2, device=DEV), torch.ones(1, device=DEV, dtype=torch.float64), 0.5):
+        with pytest.raises(ValueError):
+            opt.step(1e-3, 1, grad_scale=scale)
