@@ -346,8 +346,7 @@ extern "C" rtp_status rtp_adamw_create(rtp_adamw **out, const rtp_adamw_desc *d)
     int64_t block = 0, chunk = 0;
     for (int i = 0; i < d->count; ++i) {
         const rtp_adamw_tensor &t = d->tensors[i];
-        e[i] = {t.param_dev, t.grad_dev, t.master_dev, t.numel, block, chunk, (int)t.dtype, t.weight_decay,
-                aligned(t.param_dev, 16) && aligned(t.grad_dev, 16) && aligned(t.master_dev, 16), 0};
+        e[i] = {t.param_dev, t.grad_dev, t.master_dev, t.numel, block, chunk, (int)t.dtype, t.weight_decay};
         const int64_t n = (t.numel + ADAMW_CHUNK - 1) / ADAMW_CHUNK;
         std::fill(owner + chunk, owner + chunk + n, i);
         block += (t.numel + RTP_ADAMW_BLOCK - 1) / RTP_ADAMW_BLOCK;
@@ -400,7 +399,7 @@ extern "C" rtp_status rtp_adamw_step(rtp_adamw *opt, const rtp_adamw_hyper *h, c
     const char *who = "rtp_adamw_step";
     if (!opt || !h == !scalars_dev) return fail(RTP_ERR_INVALID, "%s: needs an optimizer, and either values or their place in device memory", who);
     if (!aligned(scalars_dev, 16) || !aligned(scale_dev, 4)) return fail(RTP_ERR_SHAPE, "%s: bad alignment", who);
-    AdamwArgs a{opt->entries, opt->owner, opt->chunks, opt->blocks, opt->m, opt->v, opt->exps, {}, scalars_dev, scale_dev};
+    AdamwArgs a{opt->entries, opt->owner, opt->chunks, opt->m, opt->v, opt->exps, {}, scalars_dev, scale_dev};
     if (h) RTP_TRY(rtp_adamw_scalars_of(h, &a.sc));
     HIP_TRY(launch_adamw(opt->moments, a, (hipStream_t)stream));
     return RTP_OK;

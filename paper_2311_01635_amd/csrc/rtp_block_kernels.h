@@ -42,13 +42,11 @@ struct AdamwEntry {
     int64_t chunk;   // its first chunk among all
     int dtype;
     float weight_decay;
-    int wide;        // all three pointers are multiples of 16 bytes
-    int pad;
 };
 struct AdamwArgs {
     const AdamwEntry *entries;
     const int32_t *owner;  // chunk -> entry
-    int64_t chunks, blocks;
+    int64_t chunks;
     void *m, *v;
     uint8_t *exps;
     rtp_adamw_scalars sc;
