@@ -282,6 +282,38 @@ def test_gradient_by_differences():
         assert abs(along - slope) <= (4 * q.c + 10 * U + 1e-7) * mags
 
 
+@pytest.mark.parametrize("D", [96, 1000, 17000])
+def test_any_of_the_parameter_gradients_alone(D):
+    """through the C ABI: each gradient by itself, and all but it, are those of the call that asks for all; the others stay as they were"""
+    import ctypes as C
+
+    from paper_2311_01635_amd import binding as B
+    q = Problem(300 if D < 2000 else 5, D, "layer", (BF16, BF16), PARTS[0]).forward().backward()
+    full = {k: v.clone() for k, v in q.grads.items()}
+    keep = [t.to(DEV) for t in (q.dr, q.dh)]
+    names = {"w_post": "dw_post_dev", "b_post": "db_post_dev", "w_pre": "dw_pre_dev", "b_pre": "db_pre_dev", "gate": "dgate_dev"}
+    d = B.rtp_norm_desc.from_buffer_copy(q.norm.desc)
+    d.T = q.T
+    ws = torch.empty(B.lib.rtp_norm_ws_bytes(C.byref(d)), dtype=torch.uint8, device=DEV)
+    for name in names:
+        for wanted in ([name], [n for n in names if n != name]):
+            g = B.rtp_norm_grads()
+            g.r_dev, g.y_dev, g.dr_dev, g.dh_dev, g.stats_dev = (t.data_ptr() for t in (q.r, q.yd, *keep, q.stats))
+            g.dx_dev, g.dy_dev, g.ws_dev, g.ws_bytes = q.dx.data_ptr(), q.dy.data_ptr(), ws.data_ptr(), ws.numel()
+            got = {n: torch.full((D,), 4.0, device=DEV) for n in names}
+            for n in wanted:
+                setattr(g, names[n], got[n].data_ptr())
+            B.check(B.lib.rtp_norm_bwd(C.byref(d), C.byref(g), torch.cuda.current_stream().cuda_stream))
+            assert all(torch.equal(got[n], full[n]) if n in wanted else (got[n] == 4.0).all() for n in names), wanted
+
+
+def test_an_element_gate_without_its_gradient():
+    q = Problem(9, 264, "rms", (BF16, BF16), PARTS[1]).forward().backward()
+    dx, dy = torch.empty_like(q.dx), torch.empty_like(q.dy)
+    q.norm.backward(q.r, q.yd, q.dr.to(DEV), q.dh.to(DEV), dx, dy, q.stats, gate=q.gd)
+    assert torch.equal(dx, q.dx) and torch.equal(dy, q.dy)
+
+
 def test_refusals_on_the_device():
     n = RtpNorm(16, post=True, w_pre=torch.ones(16, device=DEV))
     t = lambda *s, dt=BF16: torch.zeros(*s, dtype=dt, device=DEV)   # noqa: E731

@@ -4,6 +4,7 @@ Tolerances.  u = 2^-24 is half an fp32 step.  An exponential of l - m carries th
 value, and one of its own; a sum of n positive numbers at most n u; so a weight is within (R + 2 k + 12) u of itself, R the
 largest |l - m| (and of log sigmoid, which is as large).  16-bit outputs: half a step of the type on top."""
 import math
+import random
 
 import pytest
 import torch
@@ -116,6 +117,25 @@ def test_near_ties_are_decided_in_64_bits():
     bias[5] = 2.0 ** -41
     _, ids, _ = _run(l.to(DEV), 3, bias.to(DEV), score="sigmoid")
     assert ids.cpu().tolist() == [[37, 5, 0]] * 8
+
+
+@pytest.mark.parametrize("seed", range(40))
+def test_configurations(seed):
+    """any number of experts, groups and choices together"""
+    r = random.Random(seed)
+    groups = r.choice([1, 2, 3, 4, 7, 8, 16, 33, 64])
+    E = groups * r.randint(1, max(1, (16, 64, 256, 1024)[seed % 4] // groups))
+    kept = r.randint(1, groups)
+    k = r.randint(1, min(32, E // groups * kept))
+    kw = dict(score=r.choice(["softmax", "sigmoid"]), renorm=r.random() < 0.5, scale=r.choice([1.0, 2.5]), groups=groups, kept=kept, group_top=r.choice([1, 2]))
+    dtype = r.choice([F32, BF16, F16])
+    T = r.randint(1, 70)
+    l = _logits(T, E, dtype, seed, closed=r.choice([0.0, 0.5, 0.97]))
+    bias = 0.1 * torch.randn(E, generator=torch.Generator().manual_seed(seed)) if r.random() < 0.5 else None
+    _, ids, w = _run(l.to(DEV), k, None if bias is None else bias.to(DEV), **kw)
+    want_ids, want_w = ref.route(l, k, bias=bias, **kw)
+    assert torch.equal(ids.cpu(), want_ids), (T, E, k, kw)
+    assert ((w.cpu().double() - want_w).abs() <= (_tol(l, k) + (E / 64 + 16) * U) * want_w.abs()).all()
 
 
 @pytest.mark.parametrize("score", ["softmax", "sigmoid"])
