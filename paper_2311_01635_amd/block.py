@@ -229,14 +229,16 @@ class RtpNorm:
             if gate is None:
                 raise ValueError("dgate without an element gate")
             dg_p, ld_dg = _rows(dgate, "dgate", U, T, D, dev)
-        ws = None
+        ws, need = None, 0
         if self.grads:
-            if self._ws[0] != T:
-                self._ws = T, B.lib.rtp_norm_ws_bytes(C.byref(d))
+            of, need = self._ws
+            if of != T:
+                need = B.lib.rtp_norm_ws_bytes(C.byref(d))
+                self._ws = T, need
             # (a block of torch's allocator: ordered with this stream, and the graph's own while one is captured)
-            ws = torch.empty(self._ws[1], dtype=torch.uint8, device=dev)
+            ws = torch.empty(need, dtype=torch.uint8, device=dev)
         g = B.rtp_norm_grads(r_p, y_p, dr_p, dh_p, st_p, dx_p, dy_p, dg_p, *self._dparams, 1 if accumulate else 0, None if ws is None else ws.data_ptr(),
-                             self._ws[1], ld_r, ld_y, ld_dr, ld_dh, ld_dx, ld_dy, ld_dg)
+                             need, ld_r, ld_y, ld_dr, ld_dh, ld_dx, ld_dy, ld_dg)
         _call(_norm_bwd, "rtp_norm_bwd", dev, C.byref(d), C.byref(g))
         return self.grads
 

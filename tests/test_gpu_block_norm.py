@@ -307,6 +307,16 @@ def test_any_of_the_parameter_gradients_alone(D):
             assert all(torch.equal(got[n], full[n]) if n in wanted else (got[n] == 4.0).all() for n in names), wanted
 
 
+def test_batches_of_changing_size():
+    """one object, one batch after another of another number of rows: each call has the workspace of its own"""
+    for T in (700, 3, 5000, 1, 700):
+        q = Problem(T, 96, "rms", (BF16, BF16), PARTS[0])
+        if T == 700:
+            first = q
+        q.norm, q.p = first.norm, first.p
+        q.forward().backward(accumulate=False).check_backward()
+
+
 def test_an_element_gate_without_its_gradient():
     q = Problem(9, 264, "rms", (BF16, BF16), PARTS[1]).forward().backward()
     dx, dy = torch.empty_like(q.dx), torch.empty_like(q.dy)
