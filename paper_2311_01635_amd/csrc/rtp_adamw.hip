@@ -57,6 +57,15 @@ template <rtp_dtype D> __device__ __forceinline__ float round_random(float v, ui
     return copysignf(ldexpf(n, -24), v);
 }
 
+// beta x + (1 - beta) y with each product and the sum rounded by itself, as a step written out in fp32 operations does.  A fused
+// multiply-add is as near to 64 bits, but its half a unit decides a code's random rounding now and then, and the next steps go on from
+// the code: two programs that step the same state have to round alike.
+__device__ __forceinline__ float decayed(float beta, float x, float one_minus_beta, float y)
+{
+#pragma clang fp contract(off)
+    return beta * x + one_minus_beta * y;
+}
+
 // (a pointer out of the table is one into device memory: without the word for it the accesses are the flat ones, which wait for LDS too)
 template <class T> __device__ __forceinline__ T *global(T *p)
 {
@@ -128,8 +137,8 @@ __device__ __forceinline__ void adamw_blocks(const AdamwArgs &p, const AdamwEntr
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             const float gr = g[b].get(k) * scale;
-            m[k] = fmaf(h.one_minus_beta1, gr, h.beta1 * m[k]);
-            v[k] = fmaf(h.one_minus_beta2 * gr, gr, h.beta2 * v[k]);
+            m[k] = decayed(h.beta1, m[k], h.one_minus_beta1, gr);
+            v[k] = decayed(h.beta2, v[k], h.one_minus_beta2, gr * gr);
             if (BYTE || RANDOM) rnd[k] = hash(x + k * PLACE);
             // the hardware's root and reciprocal, 1 ulp each (a second moment below 2^-126 counts as zero here)
             const float d = m[k] * __builtin_amdgcn_rcpf(fmaf(__builtin_amdgcn_sqrtf(v[k]), h.root_scale, h.eps));
