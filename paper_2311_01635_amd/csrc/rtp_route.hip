@@ -360,7 +360,13 @@ __global__ __launch_bounds__(64 * RW) void route_fwd_kernel(RouteArgs p)
             wave_fence();
             for (int j = l; j < k; j += LANES) {
                 int better = 0;
-                for (int o = 0; o < k; ++o) better += c[o] > c[j] || (c[o] == c[j] && ids[o] < ids[j]);
+                for (int o = 0; o < k; ++o) {
+                    better += c[o] > c[j] || (c[o] == c[j] && ids[o] < ids[j]);
+                    // (Logits stand for their softmax here, whose probabilities are above 2^-80, so that l - top is off by 2^-47 in 64
+                    // bits, and two are in the order of their logits if these are 2^-44 apart.  Nearer ones may be equal there: the whole
+                    // row says.)
+                    unsure |= softmax && !p.bias && c[o] != c[j] && fabs(c[o] - c[j]) < 0x1p-44;
+                }
                 sorted[better] = ids[j];
             }
             wave_fence();
