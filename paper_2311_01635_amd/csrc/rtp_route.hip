@@ -511,8 +511,9 @@ __global__ __launch_bounds__(64 * RW) void route_bwd_kernel(RouteArgs p)
                 if (softmax && !renorm) {
                     d = open ? expf(v[e] - m) / z * (g[e] - dot) : 0.0f;
                 } else if (open && n[e] > 0.0f) {
-                    const float sig = 1.0f / (1.0f + expf(-v[e]));
-                    d = renorm ? expf(lg(v[e]) - m) / z * (g[e] - n[e] * dot) * (softmax ? 1.0f : 1.0f - sig) : sig * (1.0f - sig) * g[e];
+                    // (1 - s is the sigmoid of -l: of s itself nothing would be left of it from l = 17 on)
+                    const float sig = 1.0f / (1.0f + expf(-v[e])), rest = 1.0f / (1.0f + expf(v[e]));
+                    d = renorm ? expf(lg(v[e]) - m) / z * (g[e] - n[e] * dot) * (softmax ? 1.0f : rest) : sig * rest * g[e];
                 }
                 o[e] = p.d.scale * d;
             }
