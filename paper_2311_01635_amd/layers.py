@@ -297,6 +297,7 @@ class RtpMoe(_PassStreams):
         self.n, self.rank, self.act, self.mode, self.dtype = n, rank, act, mode, dtype
         self.tokens, self.combine = T, RtpCombine(top_k)
         self.xk = self.yk = self.gk = None         # rows of the slots, made when a weighted call needs them
+        self.has_yk = False                        # whether yk is of the last forward pass
         T = self.T = T * top_k
         self.gated = act == B.RTP_ACT_SWIGLU
         self.shapes = [tuple(w.shape) for w in experts[0]]
@@ -358,6 +359,7 @@ class RtpMoe(_PassStreams):
         k = self.combine.k
         if k == 1 and weights is None:
             self._forward(X, route, Y)
+            self.has_yk = False
             return
         if tuple(route.shape) != (self.tokens, k) or route.dtype != torch.int32 or not route.is_contiguous():
             raise ValueError(f"route must be a contiguous [{self.tokens}, {k}] tensor of int32")
@@ -369,6 +371,7 @@ class RtpMoe(_PassStreams):
             if k > 1:
                 self.combine.expand(X, self.xk)
             self._forward(self.xk if k > 1 else X, route, self.yk)
+            self.has_yk = True
             self.combine.forward(self.yk, weights, Y)
         self._leave()
 
@@ -378,8 +381,8 @@ class RtpMoe(_PassStreams):
         if k == 1 and weights is None and dweights is None:
             self._backward(dY, dX)
             return
-        if dweights is not None and self.yk is None:
-            raise ValueError("the forward pass had no weights")
+        if dweights is not None and not self.has_yk:
+            raise ValueError("the last forward pass had no weights")
         self.gk = self._slots(self.gk, self.O2)
         if k > 1:
             self.xk = self._slots(self.xk, self.I)      # (the layer keeps its own grouped copy of the forward pass's rows)

@@ -1,0 +1,45 @@
+"""Calls of the weighted expert layer that it refuses."""
+import pytest
+import torch
+
+import rtp_workloads as wl
+from paper_2311_01635_amd import binding as B
+from paper_2311_01635_amd.layers import RtpMoe
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+BF, F32 = torch.bfloat16, torch.float32
+T, I, O, N = 64, 128, 192, 3
+
+
+def _layer(k):
+    inp = wl.make_moe_inputs(T, I, O, I, N, seed=4)
+    return RtpMoe([tuple(torch.as_tensor(m).to(DEV, BF) for m in ex) for ex in inp["experts"]], T, 1, B.RTP_ACT_GELU_ERF, top_k=k)
+
+
+class Call:
+    def __init__(self, k, seed=0):
+        g = torch.Generator(device=DEV).manual_seed(seed)
+        self.X, self.dY = (torch.randn(T, I, generator=g, device=DEV).to(BF) for _ in range(2))
+        self.ids = torch.stack([torch.randperm(N, generator=g, device=DEV)[:k] for _ in range(T)]).int()
+        self.w, self.dw = torch.rand(T, k, generator=g, device=DEV), torch.zeros(T, k, device=DEV)
+        self.Y, self.dX = torch.zeros(T, I, dtype=BF, device=DEV), torch.zeros(T, I, dtype=BF, device=DEV)
+
+
+def test_gradient_of_weights_that_the_last_forward_pass_had_not():
+    """an earlier weighted pass has left rows behind, but they are of another batch"""
+    moe, a, b = _layer(1), Call(1, 1), Call(1, 2)
+    with pytest.raises(ValueError):
+        moe.backward(a.dY, a.dX, a.w, a.dw)                   # no pass at all
+    moe.forward(a.X, a.ids, a.Y, a.w)
+    moe.backward(a.dY, a.dX, a.w, a.dw)
+    moe.forward(b.X, b.ids, b.Y)
+    with pytest.raises(ValueError):
+        moe.backward(b.dY, b.dX, None, b.dw)
+    moe.backward(b.dY, b.dX)                                  # (the pass is still there)
+    moe.forward(b.X, b.ids, b.Y, b.w)
+    moe.backward(b.dY, b.dX, b.w, b.dw)
+    moe.sync()
+    want = (b.dY.double() * moe.yk.double()).sum(1)
+    assert float(b.dw.abs().max()) > 0 and ((b.dw[:, 0].double() - want).abs() <= 1e-5 * (b.dY.double() * moe.yk.double()).abs().sum(1)).all()
+    moe.close()
