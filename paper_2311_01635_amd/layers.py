@@ -6,7 +6,7 @@ import ctypes as C
 import torch
 
 from . import binding as B
-from .block import RtpCombine
+from .block import RtpCombine, _rows, _whole
 
 _TORCH_DT = {B.RTP_F32: torch.float32, B.RTP_BF16: torch.bfloat16, B.RTP_F16: torch.float16}
 
@@ -361,19 +361,22 @@ class RtpMoe(_PassStreams):
             self._forward(X, route, Y)
             self.has_yk = False
             return
-        if tuple(route.shape) != (self.tokens, k) or route.dtype != torch.int32 or not route.is_contiguous():
-            raise ValueError(f"route must be a contiguous [{self.tokens}, {k}] tensor of int32")
+        self._check((X, "X", self.I, k == 1), (Y, "Y", self.O2, False))
+        _whole(route, "route", torch.int32, (self.tokens, k), self.home_w.device)
+        self._check_weights(weights, "weights")
         self.yk = self._slots(self.yk, self.O2)
         if k > 1:
             self.xk = self._slots(self.xk, self.I)
         self._enter()
-        with torch.cuda.stream(self.compute_stream):    # (where the slots' rows are read and written by every pass, in order)
-            if k > 1:
-                self.combine.expand(X, self.xk)
-            self._forward(self.xk if k > 1 else X, route, self.yk)
-            self.has_yk = True
-            self.combine.forward(self.yk, weights, Y)
-        self._leave()
+        try:
+            with torch.cuda.stream(self.compute_stream):    # (where the slots' rows are read and written by every pass, in order)
+                if k > 1:
+                    self.combine.expand(X, self.xk)
+                self._forward(self.xk if k > 1 else X, route, self.yk)
+                self.has_yk = True
+                self.combine.forward(self.yk, weights, Y)
+        finally:
+            self._leave()
 
     def backward(self, dY, dX, weights=None, dweights=None):
         """weights: those of forward().  dweights (fp32 [T, top_k], or None): their gradient."""
@@ -383,16 +386,35 @@ class RtpMoe(_PassStreams):
             return
         if dweights is not None and not self.has_yk:
             raise ValueError("the last forward pass had no weights")
+        self._check((dY, "dY", self.O2, False), (dX, "dX", self.I, k == 1))
+        self._check_weights(weights, "weights")
+        self._check_weights(dweights, "dweights")
         self.gk = self._slots(self.gk, self.O2)
         if k > 1:
             self.xk = self._slots(self.xk, self.I)      # (the layer keeps its own grouped copy of the forward pass's rows)
         self._enter()
-        with torch.cuda.stream(self.compute_stream):
-            self.combine.backward(dY, self.yk if dweights is not None else None, weights, self.gk, dweights)
-            self._backward(self.gk, self.xk if k > 1 else dX)
-            if k > 1:
-                self.combine.forward(self.xk, None, dX)
-        self._leave()
+        try:
+            with torch.cuda.stream(self.compute_stream):
+                self.combine.backward(dY, self.yk if dweights is not None else None, weights, self.gk, dweights)
+                self._backward(self.gk, self.xk if k > 1 else dX)
+                if k > 1:
+                    self.combine.forward(self.xk, None, dX)
+        finally:
+            self._leave()
+
+    # A weighted call is several of the library's: every tensor is looked at before the first of them, so that it is refused as a
+    # whole.  (`whole`: the layer itself takes the matrix, which has no leading dimension there.)
+    def _check(self, *tensors):
+        dt, dev = _TORCH_DT[self.dtype], self.home_w.device
+        for t, name, cols, whole in tensors:
+            if whole:
+                _whole(t, name, dt, (self.tokens, cols), dev)
+            else:
+                _rows(t, name, dt, self.tokens, cols, dev)
+
+    def _check_weights(self, t, name):
+        if t is not None:
+            _whole(t, name, torch.float32, (self.tokens, self.combine.k), self.home_w.device)
 
     def _slots(self, buf, cols):
         return torch.empty(self.T, cols, dtype=_TORCH_DT[self.dtype], device=self.dev) if buf is None else buf

@@ -1,4 +1,4 @@
-"""Calls of the weighted expert layer that it refuses."""
+"""Calls of the weighted expert layer that it refuses: nothing has been done when they raise."""
 import pytest
 import torch
 
@@ -43,3 +43,48 @@ def test_gradient_of_weights_that_the_last_forward_pass_had_not():
     want = (b.dY.double() * moe.yk.double()).sum(1)
     assert float(b.dw.abs().max()) > 0 and ((b.dw[:, 0].double() - want).abs() <= 1e-5 * (b.dY.double() * moe.yk.double()).abs().sum(1)).all()
     moe.close()
+
+
+def _bad(t):
+    """tensors that stand in no way for `t`"""
+    yield t[:-1]
+    yield t[:, :-1]
+    yield t.to(torch.float16 if t.dtype != torch.float16 else BF)
+    yield t.cpu()
+    yield t.t().contiguous().t()
+    yield None
+
+
+@pytest.mark.parametrize("k", [1, 2])
+def test_refused_calls_leave_the_layer_as_it_was(k):
+    moe, want = _layer(k), _layer(k)
+    c, d = Call(k, 5), Call(k, 5)
+    want.forward(d.X, d.ids, d.Y, d.w)
+    want.backward(d.dY, d.dX, d.w, d.dw)
+
+    def refused(fn, **kw):
+        names = [n for n in kw if n != "weights"] + ["weights"]
+        for n in names:
+            for bad in _bad(kw[n]):
+                if (bad is None and n in ("weights", "dweights")) or (bad is not None and bad.shape == kw[n].shape and bad.dtype == kw[n].dtype and
+                                                                       bad.device == kw[n].device and bad.is_contiguous()):
+                    continue
+                with pytest.raises(ValueError):
+                    fn(**{**kw, n: bad})
+
+    before = [moe.home_w.clone(), moe.home_g.clone()]
+    refused(moe.forward, X=c.X, route=c.ids, Y=c.Y, weights=c.w)
+    moe.forward(c.X, c.ids, c.Y, c.w)
+    torch.cuda.synchronize()
+    assert torch.equal(c.Y, d.Y)
+    refused(moe.backward, dY=c.dY, dX=c.dX, weights=c.w, dweights=c.dw)
+    torch.cuda.synchronize()
+    assert torch.equal(before[0], moe.home_w) and torch.equal(before[1], moe.home_g) and (c.dX == 0).all() and (c.dw == 0).all()
+    moe.backward(c.dY, c.dX, c.w, c.dw)                       # as if nothing had been asked
+    torch.cuda.synchronize()
+    assert torch.equal(c.dX, d.dX) and torch.equal(c.dw, d.dw)
+    for got, ex in zip(moe.gathered()[1], want.gathered()[1]):
+        for x, y in zip(got, ex):
+            assert torch.equal(x, y)
+    moe.close()
+    want.close()
