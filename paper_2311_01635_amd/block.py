@@ -340,6 +340,13 @@ class RtpAdamW:
         if grad_scale is not None and not (isinstance(grad_scale, torch.Tensor) and grad_scale.numel() == 1):
             raise ValueError("grad_scale must be a tensor of one value")
         gs = None if grad_scale is None else _whole(grad_scale.reshape(1), "grad_scale", torch.float32, (1,), self.dev)
+        if self.layers:         # (what the step itself would refuse, before the layers' shards have gone home for it)
+            if not self.handle:
+                B.check(B.lib.rtp_adamw_step(None, h, sc, gs, None), "rtp_adamw_step")
+            if h is not None:
+                B.check(B.lib.rtp_adamw_scalars_of(h, C.byref(B.rtp_adamw_scalars())), "rtp_adamw_step")
+            elif sc % 16:
+                raise ValueError("scalars must be at a multiple of 16 bytes")
         for layer in self.layers:
             layer._enter()
             B.check(B.lib.rtp_ring_flush(layer.ring_handle()), "rtp_ring_flush")
