@@ -609,7 +609,8 @@ rtp_ring *rtp_moe_ring(rtp_moe *moe);
  * its kernels on `stream` (a stream of the current device, on which all
  * pointers must be) and returns.  They may be captured into a graph: no
  * allocation, no clearing by the runtime, no state between calls.  A call that
- * is refused has enqueued nothing.  Zero tokens are a call that does nothing.
+ * is refused has enqueued nothing.  Zero tokens are a call that does nothing, but
+ * for rtp_norm_bwd without `accumulate`: sums over no rows are zeros.
  * Outputs do not overlap inputs or each other except where that is said. */
 
 /* Scores a router gives its experts.  */
@@ -754,7 +755,8 @@ rtp_status rtp_norm_bwd(const rtp_norm_desc *d, const rtp_norm_grads *g, void *s
  * between rtp_ring_flush and rtp_ring_zero_grads), norms, a router's matrix.
  *   m = beta1 m + (1 - beta1) g;  v = beta2 v + (1 - beta2) g^2
  *   p = p (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v / (1 - beta2^step)) + eps)
- * in fp32; under the root a second moment below 2^-126 counts as zero.
+ * in fp32, the moments with each product and sum rounded by itself (their random
+ * rounding hangs on the last bit); under the root a second moment below 2^-126 counts as zero.
  * g: the fp32 gradient, times *scale_dev where that is given (clipping).
  * p: the fp32 master copy if there is one (the parameter is then its value,
  * rounded to nearest), else the parameter itself, 16-bit ones rounded at random

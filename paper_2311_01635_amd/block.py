@@ -3,7 +3,8 @@ combination of a token's experts, the norms, gate and residual between units, an
 
 Checks of the tensors and marshalling only; the arithmetic is librtp.so's (include/rtp.h).  As with the layers, the
 caller brings the outputs.  Every call runs on the caller's current stream, keeps nothing of its inputs and may be
-captured into a graph; tensors that come from another stream are the caller's to order.
+captured into a graph (not an optimizer's step over layers: their rings refuse a stream that is being captured).  Tensors that come
+from another stream are the caller's to order, and so are those that an object makes, on the stream it was made on.
 """
 import ctypes as C
 
@@ -313,7 +314,8 @@ class RtpAdamW:
     @classmethod
     def for_layers(cls, layers, state="f32", master=False, weight_decay=0.0, more=()):
         """Over the ring stores of rotated layers (RtpLinear, RtpMlp, RtpMoe), every slot a tensor, and `more` tensors.
-        step() then brings each layer's shards home first and clears their gradients afterwards."""
+        step() then brings each layer's shards home first and clears their gradients afterwards.  `weight_decay` is of whole
+        slots, a layer's biases among them."""
         tensors = list(more)
         for layer in layers:
             dt = {v: k for k, v in _RTP_DT.items()}[layer.dtype]

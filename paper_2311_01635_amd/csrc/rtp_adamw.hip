@@ -10,7 +10,7 @@ namespace rtp {
 // parameter's 12 bytes leave a compute unit time for 79 instructions a wave, and the hash, the update and two
 // conversions are about 70 of them.  A wave takes four blocks of 256, a lane four neighbours of each: their 16 loads are sent
 // before the first is waited for (past the caches: 752 -> 706 us for 135M with fp32 moments and masters, 5.7 TB/s), a block's largest
-// element is a reduction within the wave, and nothing needs a barrier.  135M with 8-bit moments: 282 us, 5.8 TB/s; a thread an
+// element is a reduction within the wave, and nothing needs a barrier.  135M with 8-bit moments: 295 us, 5.5 TB/s; a thread an
 // element, blocks of 256 threads: 1400.
 constexpr int AT = 256, AB = 4; // threads, blocks of a wave
 static_assert(AT / 64 * AB == ADAMW_CHUNK_BLOCKS, "a workgroup is a chunk");
@@ -59,7 +59,7 @@ template <rtp_dtype D> __device__ __forceinline__ float round_random(float v, ui
 
 // beta x + (1 - beta) y with each product and the sum rounded by itself, as a step written out in fp32 operations does.  A fused
 // multiply-add is as near to 64 bits, but its half a unit decides a code's random rounding now and then, and the next steps go on from
-// the code: two programs that step the same state have to round alike.
+// the code: two programs that step the same state have to round alike.  (Two instructions an element: 295 us instead of 294.)
 __device__ __forceinline__ float decayed(float beta, float x, float one_minus_beta, float y)
 {
 #pragma clang fp contract(off)

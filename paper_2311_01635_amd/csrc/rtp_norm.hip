@@ -35,7 +35,9 @@ struct NormFwd {
 // parameters, which would otherwise come out of L2 as often as the rows out of HBM, are fetched once, and sends for the next
 // row before it adds up the present one.  4096 rows of 4096 (fp32 stream, bf16 unit): 39 us, 5.2 TB/s.  A workgroup a row: 53 us; without
 // the next row on its way 46; loads past the caches 50; stores through them 43; 512, 1024, 1536 threads a compute unit instead of
-// 768: 39.7, 40.9, 38.9.  Two rows: 4.4 us, latency.
+// 768: 39.7, 40.9, 38.9.  Rows of 12288 and 16384: 4.9 and 5.0 TB/s.  Two rows: 4.4 us, latency.  A length just over one that fills
+// its threads leaves half of them without work, and a row's last few elements go one by one: 8192 rows (bf16) of 1024 12 us, of 1032
+// 25, of 1030 34; backward 30, 51, 85.
 
 template <int THREADS> constexpr int norm_block() { return THREADS < 256 ? 256 : THREADS; }
 
@@ -182,7 +184,7 @@ __global__ __launch_bounds__(norm_block<THREADS>()) void norm_fwd_kernel(NormFwd
 }
 
 // ---- rows of any length -------------------------------------------------------------------------------------
-// One workgroup a row, the row read once for each sum over it (rows of more than NORM_REG_D; 20000: 0.9 TB/s).
+// One workgroup a row, the row read once for each sum over it (rows of more than NORM_REG_D; 20000: 0.9 to 1.1 TB/s).
 template <rtp_dtype SD, rtp_dtype BD>
 __global__ __launch_bounds__(NT) void norm_fwd_row_kernel(NormFwd p)
 {
@@ -254,7 +256,8 @@ struct NormBwd {
 
 // Rows in registers.  Bound: HBM.  8192 rows of 8192 (bf16): 150 us, 8 of them the sums, 5.4 TB/s; without the next row on its way 190.  1990
 // rows of 768 with every part: 14 and 5 us, latency (two rows a wave, one after the other).  Rows of more than 8192 do not
-// fit 128 registers a thread and spill: 1.2 to 1.7 TB/s.  The sums over rows stay in registers too, a thread's columns over all rows of its workgroup, so
+// fit 128 registers a thread and spill: 1.2 to 1.9 TB/s.  Of 4097 to 8192 an fp32 stream spills a little with fp32 units (8192 rows of
+// 8192 3.8 TB/s, with biases 4.5) and with bf16 units and biases (4.4; without, 5.1).  The sums over rows stay in registers too, a thread's columns over all rows of its workgroup, so
 // that they cost one write a workgroup (and one read by norm_sums_kernel, which adds the workgroups up in a fixed order).
 // With k = out_scale gate w_post and q = dR k g (g: an element gate): dy = rs (q - mean q - n mean(q n)).
 template <rtp_dtype SD, rtp_dtype BD, int THREADS, int NV, bool BIAS>
@@ -263,7 +266,7 @@ __global__ __launch_bounds__(norm_block<THREADS>()) void norm_bwd_kernel(NormBwd
     using S = typename Elem<SD>::t;
     using B = typename Elem<BD>::t;
     constexpr int WAVES = THREADS / 64, ROWS = norm_block<THREADS>() / THREADS;
-    // the next row is fetched under the present one's sums where 256 registers hold both
+    // the next row is fetched under the present one's sums where 256 registers hold both (nearly: see above for fp32 on both sides)
     constexpr bool AHEAD = THREADS < 512 || (THREADS == 512 && !BIAS);
     __shared__ float2 lds[WAVES];
     const int tid = threadIdx.x % THREADS;
@@ -445,7 +448,7 @@ __global__ __launch_bounds__(norm_block<THREADS>()) void norm_bwd_kernel(NormBwd
 }
 
 // Rows of any length: a workgroup takes every gridDim.x-th row and keeps its column sums in its own part of the workspace, where each
-// column is one thread's (20000: 0.55 TB/s).
+// column is one thread's (20000: 0.4 to 0.55 TB/s).
 template <rtp_dtype SD, rtp_dtype BD>
 __global__ __launch_bounds__(NT) void norm_bwd_row_kernel(NormBwd p)
 {

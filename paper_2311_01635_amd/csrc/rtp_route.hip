@@ -6,15 +6,16 @@
 
 namespace rtp {
 
-// Bound: the arithmetic of the choice (a row of 256 is 1 KB; its eight largest are eight rounds of comparisons).  LANES lanes share
-// a row, eight or sixteen neighbouring experts each, 64 / LANES rows to a wave: a round is then a maximum over a lane's keys, one over
-// LANES lanes, and the lowest lane that has it, with no barrier and little LDS.  Keys are 32-bit integers in the order of what they
+// Bound: latency and the instructions of the choice (a row of 256 is 1 KB; its eight largest are eight rounds of comparisons).  LANES lanes
+// share a row, eight or sixteen neighbouring experts each, 64 / LANES rows to a wave: a round is then a maximum over a lane's keys, one
+// over LANES lanes, and the lowest lane that has it, with no barrier and little LDS.  Keys are 32-bit integers in the order of what they
 // stand for.  Where the choice is of scores (a bias, groups), they are scores in 32 bits; a row in which two of them that
 // matter are closer than 32 bits can tell apart is decided again in 64 bits: the chosen are put in order among themselves, or, where
 // it is in doubt who they are, the whole wave chooses again.
-// 16384 tokens over 256 experts in 8 groups, 8 a token: 28 us (all rows in 64 bits, a wave a row: 117); 23 are the 32-bit choice, of
-// which the groups 4, the rest the few rows in doubt (0.1 %), behind the last ones: 4 us to choose one again, which all of
-// them did at 30 us.  Sixteen lanes of sixteen instead of 32 of eight: 34.  8192 over 8, two a token: 4.5 us, latency.
+// 16384 tokens over 256 experts in 8 groups, 8 a token: 30 us (all rows in 64 bits, a wave a row: 117); 23 are the 32-bit choice, of
+// which the groups 4, the rest the few rows in doubt (0.1 %), behind the last ones: 4 us to choose one again.  The path that does so is
+// in the same kernel: its 123 registers (52 where the choice is of logits) and 36 KB of LDS leave four waves a SIMD to hide latency.
+// Sixteen lanes of sixteen instead of 32 of eight: 34.  8192 over 8, two a token: 4.5 us, latency.
 constexpr int RW = 4; // waves of a workgroup
 
 struct RouteArgs {
